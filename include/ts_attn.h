@@ -320,6 +320,84 @@ int ts_spec_accept(int32_t num_seqs, int32_t vocab, int32_t max_draft, const flo
                    const float *u_accept, const float *u_sample, int32_t *num_accepted,
                    int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- chunks of new tokens -----------------------------------------------------
+ * A prompt, a partial rollout resumed on another replica or a tool's reply is
+ * a chunk of new tokens behind a cached context, of any length; a continuous
+ * batch mixes chunks with sequences that decode one token.  Rows are packed:
+ * sequence b owns rows q_starts[b] .. q_starts[b + 1] - 1 of the token
+ * tensors (Q_b of them; q_starts int32 [num_seqs + 1], not decreasing), and
+ * ctx_lens[b] = L_b counts them: row i of a sequence is at position
+ * L_b - Q_b + i.  Rows outside every sequence (behind q_starts[num_seqs]) are
+ * neither read nor written.  A token tensor's row holds heads x head_dim
+ * contiguous bf16 values, rows are `stride` elements apart (a multiple of 8,
+ * so that q, k and v can be views of one projection's output), and pointers
+ * are 16-byte aligned.  Pages, page table and lengths are those of
+ * ts_decode_attn.  The calls are asynchronous on `stream`, allocate nothing
+ * and read no device data on the host.  No array content makes them access
+ * memory out of bounds: starts are clamped to [0, num_tokens], lengths to the
+ * page table; a page id outside [0, num_pages) reads as zeros and is not
+ * written. */
+typedef struct ts_chunk_shape {
+    int32_t num_seqs;           /* 1 .. 4096 */
+    int32_t num_tokens;         /* rows of the token tensors, 0 .. 2^22 */
+    int32_t num_q_heads;        /* up to 1024, a multiple of num_kv_heads, */
+    int32_t num_kv_heads;       /* with 1 .. 16 query heads per KV head */
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t page_size;          /* 16 */
+    int32_t max_q_len;          /* the longest chunk (upper bound), at most num_tokens */
+    int32_t max_pages_per_seq;  /* 1 .. 2^26 */
+    int32_t max_ctx_len;        /* upper bound on ctx_lens; sizes the worker count only */
+    int32_t num_workers;        /* 0: chosen by the library; the result does not depend on it
+                                   beyond rounding */
+    int64_t num_pages;
+} ts_chunk_shape;
+
+/* Head norms, position rotation and append to the paged cache in one pass.
+ * For row r of a sequence at position t, head by head:
+ *   x = q[r][h][:] or k[r][g][:]; if its norm weight w is given,
+ *   x <- x * w / sqrt(mean(x^2) + eps);
+ *   the pairs (x_j, x_{j + rot_dim / 2}) (interleaved: (x_{2j}, x_{2j + 1})),
+ *   j < rot_dim / 2, turn by the angle t * inv_freq[j]:
+ *     (a, b) <- (a cos - b sin, b cos + a sin);
+ *   q_out[r][h][:] = x for queries;
+ *   k_pages[page_table[b][t / 16]][g][t % 16][:] = x for keys, and
+ *   v_pages[...] = v[r][g][:] unchanged.
+ * float32 throughout, angles reduced in float64, one rounding to bf16.
+ * q_out may be q itself (with the same stride).  A row whose position or page
+ * id falls outside the pool writes its query, but no key or value.
+ *   inv_freq        float32 [rot_dim / 2] (may be NULL if rot_dim is 0)
+ *   q_norm, k_norm  bf16 [head_dim], or NULL: no norm
+ * Uses every field of the shape but max_q_len, max_ctx_len and num_workers. */
+typedef struct ts_rope_config {
+    int32_t rot_dim;            /* rotated dimensions: a multiple of 16, 0 .. head_dim */
+    int32_t interleaved;        /* 0: halves form the pairs, 1: neighbours do */
+    float eps;                  /* of the norms */
+    int32_t reserved;           /* 0 */
+    int64_t q_stride, k_stride, v_stride, q_out_stride;   /* elements between rows */
+} ts_rope_config;
+
+int ts_rope_append(const ts_chunk_shape *shape, const ts_rope_config *cfg, const void *q, const void *k,
+                   const void *v, void *q_out, void *k_pages, void *v_pages, const int32_t *page_table,
+                   const int32_t *ctx_lens, const int32_t *q_starts, const float *inv_freq,
+                   const void *q_norm, const void *k_norm, void *stream);
+
+/* Attention of the chunks over the paged cache, which holds their keys and
+ * values already: the definition of ts_decode_attn with any number of rows per
+ * sequence,
+ *   out[r][h][:] = sum_t softmax_t(scale * <q[r][h][:], K_t>) V_t,
+ *   t in [0, L_b - Q_b + i].
+ * Rows that see no key (Q_b > L_b) get zeros.  Keys and values that a row does
+ * not see do not enter its result, also where they are infinite or NaN.
+ * `workspace` is device memory of at least ts_chunk_attn_workspace_size bytes,
+ * 256-byte aligned, with any contents; calls that may run concurrently need
+ * distinct ones. */
+size_t ts_chunk_attn_workspace_size(const ts_chunk_shape *shape);
+
+int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, const void *k_pages,
+                  const void *v_pages, const int32_t *page_table, const int32_t *ctx_lens,
+                  const int32_t *q_starts, void *out, int64_t out_stride, float scale, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
 /* ---- replica completion-time model ------------------------------------------
  * Host-only (no GPU needed).  The paper turns the measured per-token decoding
  * time tau(b) = 1 / v(b) at active batch b (Sec. 2.1) into rollout time under

@@ -46,6 +46,19 @@ class AttnPlan(ctypes.Structure):
                 ("lds_bytes", ctypes.c_int64), ("workspace_bytes", ctypes.c_int64)]
 
 
+class ChunkShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_q_len", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+                ("max_ctx_len", ctypes.c_int32), ("num_workers", ctypes.c_int32), ("num_pages", ctypes.c_int64)]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64)]
+
+
 class SweepConfig(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("num_batches", ctypes.c_int32),
@@ -71,7 +84,8 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_synth_page_table", "ts_copy_bytes", "ts_stream_read", "ts_page_gather_read", "ts_event_create", "ts_event_destroy",
            "ts_event_record", "ts_event_elapsed_ms", "ts_status_string", "ts_last_error",
            "ts_version", "ts_tau_table", "ts_replica_time", "ts_request_shares", "ts_step_makespan",
-           "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept"]
+           "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
+           "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn"]
 
 
 def _load() -> ctypes.CDLL:
@@ -137,6 +151,13 @@ def _load() -> ctypes.CDLL:
     lib.ts_spec_accept_workspace_size.restype = SZ
     lib.ts_spec_accept.argtypes = [I32, I32, I32, P, P, P, P, P, P, P, P, P, SZ, P]
     lib.ts_spec_accept.restype = ctypes.c_int
+    pchunk = ctypes.POINTER(ChunkShape)
+    lib.ts_rope_append.argtypes = [pchunk, ctypes.POINTER(RopeConfig)] + [P] * 13
+    lib.ts_rope_append.restype = ctypes.c_int
+    lib.ts_chunk_attn_workspace_size.argtypes = [pchunk]
+    lib.ts_chunk_attn_workspace_size.restype = SZ
+    lib.ts_chunk_attn.argtypes = [pchunk, P, I64, P, P, P, P, P, P, I64, ctypes.c_float, P, SZ, P]
+    lib.ts_chunk_attn.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
     lib.ts_status_string.restype = ctypes.c_char_p
     lib.ts_last_error.argtypes = []
@@ -444,4 +465,100 @@ def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, 
                              next_token.data_ptr(), workspace.data_ptr(),
                              workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
           "ts_spec_accept")
+    return workspace
+
+
+# ---- chunks of new tokens (packed rows) ---------------------------------------
+
+def _rows(t, name: str) -> int:
+    """Row stride of a packed token tensor [T][heads][D]: heads contiguous."""
+    import torch
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
+    # the stride of a single row is never used; torch may report any value
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _check_paged(tensors, k_pages, v_pages, page_table, ctx_lens, q_starts):
+    import torch
+    for name, t, dt in (("k_pages", k_pages, torch.bfloat16), ("v_pages", v_pages, torch.bfloat16),
+                        ("page_table", page_table, torch.int32), ("ctx_lens", ctx_lens, torch.int32),
+                        ("q_starts", q_starts, torch.int32)):
+        if t.dtype != dt or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} tensor")
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must be [num_pages][kv_heads][16][head_dim], of one shape")
+    if page_table.dim() != 2 or ctx_lens.shape != page_table.shape[:1] or q_starts.shape != (ctx_lens.numel() + 1,):
+        raise ValueError("page_table must be [B][max_pages], ctx_lens [B] and q_starts [B + 1]")
+    _check_device(*tensors, k_pages, v_pages, page_table, ctx_lens, q_starts)
+
+
+def _check_device(*tensors):
+    """Every tensor lives on the current device, whose stream the call uses."""
+    import torch
+    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"every tensor must be on the current CUDA device ({dev}), one is on {t.device}")
+
+
+def chunk_shape_of(q, k_pages, page_table, max_q_len: Optional[int] = None, max_ctx_len: Optional[int] = None,
+                   num_workers: int = 0) -> ChunkShape:
+    T, Hq, D = q.shape
+    NP, Hkv, P, D2 = k_pages.shape
+    if D != D2:
+        raise ValueError("q and k_pages head_dim differ")
+    B, maxp = page_table.shape
+    return ChunkShape(B, T, Hq, Hkv, D, P, T if max_q_len is None else int(max_q_len), maxp,
+                      maxp * P if max_ctx_len is None else int(max_ctx_len), num_workers, NP)
+
+
+def chunk_workspace_size(shape: ChunkShape) -> int:
+    n = lib.ts_chunk_attn_workspace_size(ctypes.byref(shape))
+    if n == 0:
+        raise TsError(-2, "ts_chunk_attn_workspace_size")
+    return int(n)
+
+
+def rope_append(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm=None,
+                k_norm=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """ts_rope_append on torch tensors: q, q_out bf16 [T][Hq][D], k, v bf16
+    [T][Hkv][D] (rows may be strided, as views of one projection's output are),
+    inv_freq float32 [rot_dim / 2] or None, norms bf16 [D] or None."""
+    import torch
+    strides = [_rows(t, n) for n, t in (("q", q), ("k", k), ("v", v), ("q_out", q_out))]
+    _check_paged((q, k, v, q_out, inv_freq, q_norm, k_norm), k_pages, v_pages, page_table, ctx_lens, q_starts)
+    T, Hq, D = q.shape
+    if q_out.shape != q.shape or k.shape != (T, k_pages.shape[1], D) or v.shape != k.shape:
+        raise ValueError("q_out must match q, and k and v must be [tokens][kv_heads][head_dim]")
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq must be a contiguous float32 vector")
+    for n, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None and (w.dtype != torch.bfloat16 or w.shape != (D,) or not w.is_contiguous()):
+            raise ValueError(f"{n} must be a contiguous bf16 vector of head_dim values")
+    shape = chunk_shape_of(q, k_pages, page_table)
+    cfg = RopeConfig(0 if inv_freq is None else 2 * inv_freq.numel(), int(interleaved), eps, 0, *strides)
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    check(lib.ts_rope_append(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                             q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                             ctx_lens.data_ptr(), q_starts.data_ptr(), ptr(inv_freq), ptr(q_norm), ptr(k_norm),
+                             _stream_ptr(stream)), "ts_rope_append")
+
+
+def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: float, workspace=None,
+               max_q_len: Optional[int] = None, max_ctx_len: Optional[int] = None, num_workers: int = 0, stream=None):
+    """ts_chunk_attn on torch tensors (q, out: bf16 [T][Hq][D], rows may be
+    strided); returns the workspace tensor used."""
+    import torch
+    strides = _rows(q, "q"), _rows(out, "out")
+    _check_paged((q, out, workspace), k_pages, v_pages, page_table, ctx_lens, q_starts)
+    if out.shape != q.shape:
+        raise ValueError("out must match q")
+    shape = chunk_shape_of(q, k_pages, page_table, max_q_len, max_ctx_len, num_workers)
+    if workspace is None:
+        workspace = torch.empty(chunk_workspace_size(shape), dtype=torch.uint8, device=q.device)
+    check(lib.ts_chunk_attn(ctypes.byref(shape), q.data_ptr(), strides[0], k_pages.data_ptr(), v_pages.data_ptr(),
+                            page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
+                            strides[1], ctypes.c_float(scale), workspace.data_ptr(),
+                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_chunk_attn")
     return workspace
