@@ -398,6 +398,43 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
                   const int32_t *q_starts, void *out, int64_t out_stride, float scale, void *workspace,
                   size_t workspace_bytes, void *stream);
 
+/* ---- sampling ------------------------------------------------------------------
+ * Draws each sequence's next token from its row of logits l, with the rule of
+ * ts_spec_accept (the smallest token whose cumulative mass exceeds u times the
+ * total, the caller's uniform u in [0, 1)) on the weights that the filters
+ * leave of w_v = exp((l_v - max l) / temperature):
+ *   top-k (0 < k < vocab; else off)   the k largest logits;
+ *   top-p (p < 1; else or NaN off)    of those, in descending order, each with
+ *                                     less than p times their mass in front of
+ *                                     it (the first one always);
+ *   min-p (0 < m; capped at 1)        of those, the ones with w_v >= m.
+ * Equal logits rank by index, the lowest first.  A temperature that is not
+ * above 0 takes the largest logit.  logprob (may be NULL) is the natural
+ * logarithm of the probability that the drawn token had among the kept ones (0
+ * for the largest logit).  Logits of -inf and NaN have no mass, +inf reads as
+ * the largest float32; a row without mass gives token -1 and logprob -inf.
+ * Masses are integers in units of 2^-42 of the largest weight or finer, so
+ * results do not depend on the order of sums.
+ *   logits       float32 or bf16 [num_seqs][vocab], rows row_stride elements
+ *                apart (at least vocab, any alignment of an element);
+ *                num_seqs 1 .. 65536, vocab 1 .. 2^20
+ *   temperature, top_p, min_p  float32 [num_seqs], top_k  int32 [num_seqs]; each
+ *                may be NULL (temperature 1, filter off)
+ *   u            float32 [num_seqs], clamped to [0, 1 - 2^-24], NaN read as 0
+ *   token        int32 [num_seqs];  logprob  float32 [num_seqs]
+ * Asynchronous on `stream`; the workspace (ts_sample_workspace_size bytes,
+ * 256-byte aligned, any contents) carries the slices' sums between the call's
+ * two launches. */
+#define TS_LOGITS_F32 0
+#define TS_LOGITS_BF16 1
+
+size_t ts_sample_workspace_size(int32_t num_seqs, int32_t vocab);
+
+int ts_sample(int32_t num_seqs, int32_t vocab, int32_t logits_type, const void *logits,
+              int64_t row_stride, const float *temperature, const int32_t *top_k, const float *top_p,
+              const float *min_p, const float *u, int32_t *token, float *logprob, void *workspace,
+              size_t workspace_bytes, void *stream);
+
 /* ---- replica completion-time model ------------------------------------------
  * Host-only (no GPU needed).  The paper turns the measured per-token decoding
  * time tau(b) = 1 / v(b) at active batch b (Sec. 2.1) into rollout time under

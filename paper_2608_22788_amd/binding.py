@@ -37,6 +37,7 @@ class AttnShape(ctypes.Structure):
 
 
 VARIANT_AUTO, VARIANT_WAVE, VARIANT_TEAM, VARIANT_VALU = 0, 1, 2, 3
+LOGITS_F32, LOGITS_BF16 = 0, 1
 COMBINE_MERGE_KERNEL, COMBINE_LAST_ARRIVER, COMBINE_IN_LAUNCH = 0, 1, 2
 
 
@@ -85,7 +86,8 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_event_record", "ts_event_elapsed_ms", "ts_status_string", "ts_last_error",
            "ts_version", "ts_tau_table", "ts_replica_time", "ts_request_shares", "ts_step_makespan",
            "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
-           "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn"]
+           "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn",
+           "ts_sample_workspace_size", "ts_sample"]
 
 
 def _load() -> ctypes.CDLL:
@@ -158,6 +160,10 @@ def _load() -> ctypes.CDLL:
     lib.ts_chunk_attn_workspace_size.restype = SZ
     lib.ts_chunk_attn.argtypes = [pchunk, P, I64, P, P, P, P, P, P, I64, ctypes.c_float, P, SZ, P]
     lib.ts_chunk_attn.restype = ctypes.c_int
+    lib.ts_sample_workspace_size.argtypes = [I32, I32]
+    lib.ts_sample_workspace_size.restype = SZ
+    lib.ts_sample.argtypes = [I32, I32, I32, P, I64, P, P, P, P, P, P, P, P, SZ, P]
+    lib.ts_sample.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
     lib.ts_status_string.restype = ctypes.c_char_p
     lib.ts_last_error.argtypes = []
@@ -561,4 +567,40 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
                             page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
                             strides[1], ctypes.c_float(scale), workspace.data_ptr(),
                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_chunk_attn")
+    return workspace
+
+
+# ---- sampling ------------------------------------------------------------------
+
+def sample_workspace_size(num_seqs: int, vocab: int) -> int:
+    n = lib.ts_sample_workspace_size(num_seqs, vocab)
+    if n == 0:
+        raise TsError(-6, "ts_sample_workspace_size")
+    return int(n)
+
+
+def sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None,
+           stream=None):
+    """ts_sample on torch tensors: logits float32 or bf16 [B][V] (rows may be
+    strided), u float32 [B], token int32 [B], logprob float32 [B] or None, the
+    parameters one value per row or None; returns the workspace tensor used."""
+    import torch
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("logits must be a float32 or bf16 tensor [B][V] whose rows are contiguous")
+    B, V = logits.shape
+    for name, t, dt in (("u", u, torch.float32), ("token", token, torch.int32), ("logprob", logprob, torch.float32),
+                        ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is None and name not in ("u", "token"):
+            continue
+        if t.dtype != dt or t.shape != (B,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} vector with a value per row")
+    _check_device(logits, u, token, logprob, temperature, top_k, top_p, min_p, workspace)
+    if workspace is None:
+        workspace = torch.empty(sample_workspace_size(B, V), dtype=torch.uint8, device=logits.device)
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    check(lib.ts_sample(B, V, LOGITS_F32 if logits.dtype == torch.float32 else LOGITS_BF16, logits.data_ptr(),
+                        logits.stride(0) if B > 1 else V, ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p),
+                        u.data_ptr(), token.data_ptr(), ptr(logprob), workspace.data_ptr(),
+                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_sample")
     return workspace
