@@ -13,6 +13,7 @@ import os
 from typing import List, Optional, Sequence
 
 import numpy as np
+import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libtsattn.so")
@@ -475,37 +476,47 @@ def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, 
 
 
 # ---- chunks of new tokens (packed rows) ---------------------------------------
+# The smallest of these calls run for less than Python takes to check their
+# arguments attribute by attribute, so each attribute is read once.
 
-def _rows(t, name: str) -> int:
-    """Row stride of a packed token tensor [T][heads][D]: heads contiguous."""
-    import torch
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+def _rows(t, name: str):
+    """(tokens, heads, head_dim, row stride) of a packed token tensor, whose
+    heads are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or stride[1] != shape[2]:
         raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
+    T, H, D = shape
     # the stride of a single row is never used; torch may report any value
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return T, H, D, stride[0] if T > 1 else H * D
 
 
-def _check_paged(tensors, k_pages, v_pages, page_table, ctx_lens, q_starts):
-    import torch
-    for name, t, dt in (("k_pages", k_pages, torch.bfloat16), ("v_pages", v_pages, torch.bfloat16),
-                        ("page_table", page_table, torch.int32), ("ctx_lens", ctx_lens, torch.int32),
-                        ("q_starts", q_starts, torch.int32)):
-        if t.dtype != dt or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dt} tensor")
-    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts):
+    """(num_pages, kv_heads, page size, head_dim, sequences, pages per sequence)."""
+    bf16, i32 = torch.bfloat16, torch.int32
+    if (k_pages.dtype != bf16 or v_pages.dtype != bf16 or page_table.dtype != i32 or ctx_lens.dtype != i32 or
+            q_starts.dtype != i32):
+        raise ValueError("k_pages and v_pages must be bf16, page_table, ctx_lens and q_starts int32 tensors")
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous() and
+            ctx_lens.is_contiguous() and q_starts.is_contiguous()):
+        raise ValueError("k_pages, v_pages, page_table, ctx_lens and q_starts must be contiguous")
+    pool, table = k_pages.shape, page_table.shape
+    if len(pool) != 4 or v_pages.shape != pool:
         raise ValueError("k_pages and v_pages must be [num_pages][kv_heads][16][head_dim], of one shape")
-    if page_table.dim() != 2 or ctx_lens.shape != page_table.shape[:1] or q_starts.shape != (ctx_lens.numel() + 1,):
+    if len(table) != 2 or ctx_lens.shape != table[:1] or q_starts.shape != (table[0] + 1,):
         raise ValueError("page_table must be [B][max_pages], ctx_lens [B] and q_starts [B + 1]")
-    _check_device(*tensors, k_pages, v_pages, page_table, ctx_lens, q_starts)
+    return (*pool, *table)
 
 
-def _check_device(*tensors):
+def _check_device(*tensors) -> None:
     """Every tensor lives on the current device, whose stream the call uses."""
-    import torch
-    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    dev = torch.cuda.current_device() if tensors[0].is_cuda else None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"every tensor must be on the current CUDA device ({dev}), one is on {t.device}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def chunk_shape_of(q, k_pages, page_table, max_q_len: Optional[int] = None, max_ctx_len: Optional[int] = None,
@@ -531,23 +542,27 @@ def rope_append(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts
     """ts_rope_append on torch tensors: q, q_out bf16 [T][Hq][D], k, v bf16
     [T][Hkv][D] (rows may be strided, as views of one projection's output are),
     inv_freq float32 [rot_dim / 2] or None, norms bf16 [D] or None."""
-    import torch
-    strides = [_rows(t, n) for n, t in (("q", q), ("k", k), ("v", v), ("q_out", q_out))]
-    _check_paged((q, k, v, q_out, inv_freq, q_norm, k_norm), k_pages, v_pages, page_table, ctx_lens, q_starts)
-    T, Hq, D = q.shape
-    if q_out.shape != q.shape or k.shape != (T, k_pages.shape[1], D) or v.shape != k.shape:
+    T, Hq, D, q_stride = _rows(q, "q")
+    Tk, Hk, Dk, k_stride = _rows(k, "k")
+    Tv, Hv, Dv, v_stride = _rows(v, "v")
+    To, Ho, Do, out_stride = _rows(q_out, "q_out")
+    NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts)
+    if not (T == Tk == Tv == To and Hq == Ho and Hkv == Hk == Hv and D == Dk == Dv == Do == Dp):
         raise ValueError("q_out must match q, and k and v must be [tokens][kv_heads][head_dim]")
-    if inv_freq is not None and (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous()):
-        raise ValueError("inv_freq must be a contiguous float32 vector")
+    rot = 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float32 vector")
     for n, w in (("q_norm", q_norm), ("k_norm", k_norm)):
         if w is not None and (w.dtype != torch.bfloat16 or w.shape != (D,) or not w.is_contiguous()):
             raise ValueError(f"{n} must be a contiguous bf16 vector of head_dim values")
-    shape = chunk_shape_of(q, k_pages, page_table)
-    cfg = RopeConfig(0 if inv_freq is None else 2 * inv_freq.numel(), int(interleaved), eps, 0, *strides)
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    _check_device(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm)
+    shape = ChunkShape(B, T, Hq, Hkv, D, P, T, maxp, maxp * P, 0, NP)
+    cfg = RopeConfig(rot, int(interleaved), eps, 0, q_stride, k_stride, v_stride, out_stride)
     check(lib.ts_rope_append(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                              q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                             ctx_lens.data_ptr(), q_starts.data_ptr(), ptr(inv_freq), ptr(q_norm), ptr(k_norm),
+                             ctx_lens.data_ptr(), q_starts.data_ptr(), _ptr(inv_freq), _ptr(q_norm), _ptr(k_norm),
                              _stream_ptr(stream)), "ts_rope_append")
 
 
@@ -555,17 +570,19 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
                max_q_len: Optional[int] = None, max_ctx_len: Optional[int] = None, num_workers: int = 0, stream=None):
     """ts_chunk_attn on torch tensors (q, out: bf16 [T][Hq][D], rows may be
     strided); returns the workspace tensor used."""
-    import torch
-    strides = _rows(q, "q"), _rows(out, "out")
-    _check_paged((q, out, workspace), k_pages, v_pages, page_table, ctx_lens, q_starts)
-    if out.shape != q.shape:
-        raise ValueError("out must match q")
-    shape = chunk_shape_of(q, k_pages, page_table, max_q_len, max_ctx_len, num_workers)
+    T, Hq, D, q_stride = _rows(q, "q")
+    To, Ho, Do, out_stride = _rows(out, "out")
+    NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts)
+    if not (T == To and Hq == Ho and D == Do == Dp):
+        raise ValueError("out must match q, and head_dim that of the pages")
+    _check_device(q, out, k_pages, v_pages, page_table, ctx_lens, q_starts, workspace)
+    shape = ChunkShape(B, T, Hq, Hkv, D, P, T if max_q_len is None else int(max_q_len), maxp,
+                       maxp * P if max_ctx_len is None else int(max_ctx_len), num_workers, NP)
     if workspace is None:
         workspace = torch.empty(chunk_workspace_size(shape), dtype=torch.uint8, device=q.device)
-    check(lib.ts_chunk_attn(ctypes.byref(shape), q.data_ptr(), strides[0], k_pages.data_ptr(), v_pages.data_ptr(),
+    check(lib.ts_chunk_attn(ctypes.byref(shape), q.data_ptr(), q_stride, k_pages.data_ptr(), v_pages.data_ptr(),
                             page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
-                            strides[1], ctypes.c_float(scale), workspace.data_ptr(),
+                            out_stride, scale, workspace.data_ptr(),
                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_chunk_attn")
     return workspace
 
@@ -584,23 +601,20 @@ def sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=N
     """ts_sample on torch tensors: logits float32 or bf16 [B][V] (rows may be
     strided), u float32 [B], token int32 [B], logprob float32 [B] or None, the
     parameters one value per row or None; returns the workspace tensor used."""
-    import torch
     if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits must be a float32 or bf16 tensor [B][V] whose rows are contiguous")
     B, V = logits.shape
+    rows = (B,)
     for name, t, dt in (("u", u, torch.float32), ("token", token, torch.int32), ("logprob", logprob, torch.float32),
                         ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                         ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if t is None and name not in ("u", "token"):
-            continue
-        if t.dtype != dt or t.shape != (B,) or not t.is_contiguous():
+        if t is not None and (t.dtype != dt or t.shape != rows or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous {dt} vector with a value per row")
     _check_device(logits, u, token, logprob, temperature, top_k, top_p, min_p, workspace)
     if workspace is None:
         workspace = torch.empty(sample_workspace_size(B, V), dtype=torch.uint8, device=logits.device)
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
     check(lib.ts_sample(B, V, LOGITS_F32 if logits.dtype == torch.float32 else LOGITS_BF16, logits.data_ptr(),
-                        logits.stride(0) if B > 1 else V, ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p),
-                        u.data_ptr(), token.data_ptr(), ptr(logprob), workspace.data_ptr(),
+                        logits.stride(0) if B > 1 else V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                        u.data_ptr(), token.data_ptr(), _ptr(logprob), workspace.data_ptr(),
                         workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_sample")
     return workspace

@@ -21,24 +21,34 @@
 // by block, run by run and element by element with the same integers.  A
 // weight is off by at most a unit, 2^-42 of the largest.
 //
-// What bounds it: the row is read once from memory, and a weight costs about
-// 20 float64-rate instructions (as many as float32 ones issue here), a little
-// less than the read at 4 bytes a logit.  Sequences are few and rows long, so
-//   - sample_slices_kernel spreads the rows over the chip in slices, each held
-//     in registers: its maximum, then its mass, or, for rows with top-k or
-//     top-p, how many logits and how much mass lie in bins of an eighth of a
-//     binary order below its maximum (the bins of different slices lie on one
-//     grid);
-//   - sample_pick_kernel, one workgroup per row, joins the slices and either
-//     draws (no filters), or finds the bin where a filter ends, collects the
-//     logits above its lower edge into LDS, finds the last kept one there by a
-//     radix descent over (logit, index), and draws among the kept ones.
-// Only rows whose filter leaves more than fits LDS are read again (from the
-// caches).
+// What bounds it: the row is read once from memory, and a weight costs 22
+// float64-rate instructions (as many as float32 ones issue here), about as
+// long as reading 4 bytes takes.  Sequences are few and rows long, so the work
+// on whole rows is spread over the chip in slices held in registers:
+//   - sample_slices_kernel: a slice's maximum, then its mass, or, for rows with
+//     top-k or top-p, how many logits and how much mass lie in bins of an
+//     eighth of a binary order below its maximum (the bins of different slices
+//     lie on one grid);
+//   - sample_plan_kernel, one workgroup per row, joins the slices and draws
+//     where there is no filter; else it finds the bin where the filter ends;
+// and with filters
+//   - sample_gather_kernel appends the logits from that bin on to the row's
+//     list, or, where they are too many, the bin's alone and sums the weights of
+//     what lies above it;
+//   - sample_filter_kernel, one workgroup per row, finds the last kept logit in
+//     the list (pair by pair if few, else by a radix descent over (logit,
+//     index)) and draws.
+// Measured, 151,936 logits a row: 8 float32 rows with temperature alone 14.3
+// us; 200 bf16 rows, each with its own filters, 125 us.  With one workgroup
+// reading each filtered row again instead of the two last kernels' slices that
+// was 245 us.  Only a row of which more than kList logits lie in one bin is
+// still read by one workgroup.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <climits>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "ts_attn.h"
@@ -56,18 +66,30 @@ namespace {
 constexpr int kMaxVocabBits = 20;
 constexpr int kSliceThreads = 256;
 constexpr int kSliceUnit = 16 * kSliceThreads;   // logits of a slice per pass of its registers
-constexpr int kLongSlice = 4;                    // passes of the longer slices
+constexpr int kLongSlice = 2;                    // passes of the longer slices
 constexpr int kBins = 256;
 constexpr double kBinsPerOctave = 8.0;
-constexpr int kPickThreads = 1024;
-constexpr int kPickWaves = kPickThreads / kWave;
-constexpr int kRun = 256;                        // logits per mass kept while a filtered row is summed
-constexpr int kMaxRuns = (1 << kMaxVocabBits) / kRun;
-constexpr int kList = 4096;                      // logits collected in LDS
+constexpr int kMaxSlices = (1 << kMaxVocabBits) / kSliceUnit;
+constexpr int kPlanThreads = 256, kFilterThreads = 1024;
+constexpr int kRun = 256;                        // logits that a wavefront reads at once of a whole row
+constexpr int kList = 8192;                      // candidates of a row
+constexpr int kFew = 256;                        // of them, compared pair by pair
 constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;
+
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 
 typedef unsigned long long u64;   // the type of the LDS atomics
+
+// What the filters leave to be found out about a row (see sample_plan_kernel).
+enum { kDrawn, kListed, kScanned };   // done; candidates in the list; too many of them
+struct RowPlan {
+    int state;
+    int n;                  // candidates appended to the list
+    float m;                // largest logit
+    float lo, hi;
+    bool by_count, then_p;  // a top-k ends among the candidates; then a top-p of what it keeps
+    u64 want;               // the running count or mass at which the filter ends (0: none does)
+};
 
 struct SampleParams {
     const void *logits;
@@ -80,8 +102,10 @@ struct SampleParams {
     u64 *s_mass;           // [B][slices] (rows without filters)
     uint32_t *h_count;     // [B][slices][kBins]
     u64 *h_mass;
+    RowPlan *plan;         // [B]
+    u64 *list;             // [B][list_len]
     int64_t row_stride;
-    int V, slices, slice_len;
+    int V, slices, slice_len, list_len;
 };
 
 // What a row asks for.
@@ -89,7 +113,8 @@ struct RowRule {
     bool greedy, by_k, by_p, by_min;
     double c;       // log2(e) / T
     int k;
-    float p, min_p;
+    float p;
+    double min_x;   // log2(min_p)
 };
 __device__ __forceinline__ RowRule row_rule(const SampleParams &a, int b) {
     RowRule r;
@@ -100,8 +125,9 @@ __device__ __forceinline__ RowRule row_rule(const SampleParams &a, int b) {
     r.by_k = !r.greedy && r.k > 0 && r.k < a.V;
     r.p = a.top_p ? a.top_p[b] : 1.0f;
     r.by_p = !r.greedy && r.p < 1.0f;
-    r.min_p = a.min_p ? fminf(a.min_p[b], 1.0f) : 0.0f;
-    r.by_min = !r.greedy && r.min_p > 0.0f;
+    const float min_p = a.min_p ? fminf(a.min_p[b], 1.0f) : 0.0f;
+    r.by_min = !r.greedy && min_p > 0.0f;
+    r.min_x = r.by_min ? log2((double)min_p) : 0.0;
     return r;
 }
 
@@ -140,26 +166,28 @@ __device__ __forceinline__ float one_logit(const T *row, int i) {
 // ---- weights ----------------------------------------------------------------------
 __device__ __forceinline__ double scaled(float l, double c) { return (double)l * c; }
 
-// The weight of scaled logit x in units of 2^(E - 42) (E >= rint(x)).
+// A constant in scalar registers, where the compiler would otherwise move it
+// into the accumulator of every multiply-add (two moves each).
+__device__ __forceinline__ double scalar(double k) {
+    asm("" : "+s"(k));
+    return k;
+}
+
+// The weight of scaled logit x in units of 2^(E - 42) (E >= rint(x)); 0 for the
+// -inf or NaN that x is for a logit of -inf.
 __device__ __forceinline__ u64 weight(double x, double E) {
+    constexpr double k[11] = {0x1p52 + 0x1p42, 0x1.62e42fefa39efp+41, 0x1.ebfbdff82c58ep+39, 0x1.c6b08d704a0bfp+37, 0x1.3b2ab6fba4e77p+35, 0x1.5d87fe78a6730p+32,
+                              0x1.430912f86c786p+29, 0x1.ffcbfc588b0c5p+25, 0x1.62c0223a5c822p+22, 0x1.b5253d395e7c1p+18, 0x1.e4cf5158b8ec7p+14};   // 2^42 ln(2)^i / i!
     const double n = rint(x), r = x - n;
-    double y = 0x1.e4cf5158b8ec7p+14;            // 2^42 ln(2)^k / k!, k = 10 .. 0
-    y = fma(y, r, 0x1.b5253d395e7c1p+18);
-    y = fma(y, r, 0x1.62c0223a5c822p+22);
-    y = fma(y, r, 0x1.ffcbfc588b0c5p+25);
-    y = fma(y, r, 0x1.430912f86c786p+29);
-    y = fma(y, r, 0x1.5d87fe78a6730p+32);
-    y = fma(y, r, 0x1.3b2ab6fba4e77p+35);
-    y = fma(y, r, 0x1.c6b08d704a0bfp+37);
-    y = fma(y, r, 0x1.ebfbdff82c58ep+39);
-    y = fma(y, r, 0x1.62e42fefa39efp+41);
-    // adding 2^52 leaves the integer in the significand
-    const double d = fma(y, r, 0x1p52 + 0x1p42);
-    const u64 m = (u64)__double_as_longlong(d) & ((1ull << 52) - 1);
+    double y = scalar(k[10]);
+#pragma unroll
+    for (int i = 9; i >= 0; i--)
+        y = fma(y, r, scalar(k[i]));
+    // adding 2^52 has left the integer in the significand
+    const u64 m = (u64)__double_as_longlong(y) & ((1ull << 52) - 1);
     const double s = E - n;
     return s < 64.0 ? m >> (int)s : 0;
 }
-// (a logit of -inf has no weight; callers test that)
 
 // floor(u z) and ceil(p z) for float32 u, p in [0, 1) and z < 2^63.
 __device__ __forceinline__ void fraction_of(float f, u64 z, u64 *floor_out, u64 *ceil_out) {
@@ -217,26 +245,14 @@ __device__ __forceinline__ u64 block_scan(u64 x, u64 *lds, u64 *total) {
     return before + incl;
 }
 
-// ---- slices -------------------------------------------------------------------------
-
+// The n logits of a slice, -inf past them: thread t holds kVec from index
+// (i * kSliceThreads + t) * kVec.
 template <typename T, int kPasses>
-__global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleParams a) {
-    constexpr int kVec = 16 / sizeof(T);                     // logits per load
-    constexpr int kLoads = 16 * kPasses / kVec;
-    __shared__ float red[kSliceThreads / kWave];
-    __shared__ u64 mass_of[kBins], wave_mass[kSliceThreads / kWave];
-    __shared__ uint32_t count_of[kBins];
-    __shared__ int arg;
-    const int b = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
-    const int tid = threadIdx.x;
-    const RowRule rule = row_rule(a, b);
-    const int first = slice * a.slice_len, n = min(a.V - first, a.slice_len);
-    const T *src = static_cast<const T *>(a.logits) + (int64_t)b * a.row_stride + first;
-
-    float l[kLoads][kVec];
+__device__ __forceinline__ void load_slice(const T *src, int n, float (&l)[16 * kPasses * sizeof(T) / 16][16 / sizeof(T)]) {
+    constexpr int kVec = 16 / sizeof(T), kLoads = 16 * kPasses / kVec;
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
-        const int at = (i * kSliceThreads + tid) * kVec;
+        const int at = (i * kSliceThreads + (int)threadIdx.x) * kVec;
         if (at + kVec <= n) {
             if constexpr (sizeof(T) == 4) {
                 const f4_any v = *reinterpret_cast<const f4_any *>(src + at);
@@ -255,6 +271,26 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
                 l[i][e] = at + e < n ? one_logit(src, at + e) : -INFINITY;
         }
     }
+}
+
+// ---- slices -------------------------------------------------------------------------
+
+template <typename T, int kPasses>
+__global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SampleParams a) {
+    constexpr int kVec = 16 / sizeof(T);                     // logits per load
+    constexpr int kLoads = 16 * kPasses / kVec;
+    __shared__ float red[kSliceThreads / kWave];
+    __shared__ u64 mass_of[kBins], wave_mass[kSliceThreads / kWave];
+    __shared__ uint32_t count_of[kBins];
+    __shared__ int arg;
+    const int b = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const int tid = threadIdx.x;
+    const RowRule rule = row_rule(a, b);
+    const int first = slice * a.slice_len, n = min(a.V - first, a.slice_len);
+    const T *src = static_cast<const T *>(a.logits) + (int64_t)b * a.row_stride + first;
+
+    float l[kLoads][kVec];
+    load_slice<T, kPasses>(src, n, l);
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLoads; i++)
@@ -285,13 +321,11 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
         if (rule.by_min)
             return;   // the maximum is all that the pick needs
         u64 sum = 0;
-        if (m > -INFINITY) {
 #pragma unroll
-            for (int i = 0; i < kLoads; i++)
+        for (int i = 0; i < kLoads; i++)
 #pragma unroll
-                for (int e = 0; e < kVec; e++)
-                    sum += l[i][e] > -INFINITY ? weight(scaled(l[i][e], rule.c), E) : 0;
-        }
+            for (int e = 0; e < kVec; e++)
+                sum += weight(scaled(l[i][e], rule.c), E);
         u64 total;
         block_scan<kSliceThreads / kWave>(sum, wave_mass, &total);
         if (tid == 0)
@@ -303,17 +337,29 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
     mass_of[tid] = 0;
     __syncthreads();
     const double top_bin = floor(top * kBinsPerOctave);
+    uint32_t far = 0;   // what lies in the last bin, most logits of a confident row, is summed in registers
+    u64 far_mass = 0;
 #pragma unroll
     for (int i = 0; i < kLoads; i++)
 #pragma unroll
         for (int e = 0; e < kVec; e++)
             if (l[i][e] > -INFINITY) {
                 const double x = scaled(l[i][e], rule.c);
-                const int bin = (int)fmin(top_bin - floor(x * kBinsPerOctave), (double)(kBins - 1));
-                atomicAdd(&count_of[bin], 1u);
-                if (rule.by_p)
-                    atomicAdd(&mass_of[bin], weight(x, E));
+                const double bin = top_bin - floor(x * kBinsPerOctave);
+                const u64 w = rule.by_p ? weight(x, E) : 0;
+                if (bin < kBins - 1) {
+                    atomicAdd(&count_of[(int)bin], 1u);
+                    if (rule.by_p)
+                        atomicAdd(&mass_of[(int)bin], w);
+                } else {
+                    far++;
+                    far_mass += w;
+                }
             }
+    if (far)
+        atomicAdd(&count_of[kBins - 1], far);
+    if (far_mass)
+        atomicAdd(&mass_of[kBins - 1], far_mass);
     __syncthreads();
     a.h_count[at_slice * kBins + tid] = count_of[tid];
     if (rule.by_p)
@@ -322,22 +368,28 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
 
 // ---- pick ---------------------------------------------------------------------------
 
-struct PickLds {
-    u64 list[kList];        // ranks of the collected logits
-    u64 digit[kDigits];
-    u64 run[kMaxRuns];      // kept mass of each run of logits
-    u64 waves[kPickWaves];
+// What every pick workgroup needs in LDS, and what the filters' ones need.
+struct DrawLds {
+    u64 waves[kFilterThreads / kWave];
+    float red[kFilterThreads / kWave];
+    u64 found_base;
+    int found, last;
+};
+struct PlanLds : DrawLds {
     u64 bin_mass[kBins];
     uint32_t bin_count[kBins];
-    float red[kPickWaves];
-    u64 found64, found_base;
-    int found, last, n;
+};
+struct FilterLds : DrawLds {
+    u64 list[kList];        // ranks of the candidates
+    u64 digit[kDigits];     // sums by digit; of few candidates, their weights
+    u64 slice[kMaxSlices];  // kept mass of each slice
 };
 
-// First index i of v[0 .. n) whose running sum reaches `target` (n if none), in
-// every thread; *base is the sum in front of it.  n <= kPer * threads.
-template <int kPer, typename Get>
-__device__ __forceinline__ int first_reaching(PickLds &s, int n, u64 target, u64 *base, u64 *total, Get get) {
+// First index i of the n values get(i) whose running sum reaches a target that
+// may depend on their total (n if none), in every thread; *base is the sum in
+// front of it.  n <= kPer * threads.
+template <int kThreads, int kPer, typename Get, typename Target>
+__device__ __forceinline__ int first_reaching(DrawLds &s, int n, u64 *base, u64 *total, u64 *target, Get get, Target target_of) {
     const int tid = threadIdx.x;
     u64 v[kPer], sum = 0;
 #pragma unroll
@@ -348,12 +400,13 @@ __device__ __forceinline__ int first_reaching(PickLds &s, int n, u64 target, u64
     }
     if (tid == 0)
         s.found = n;
-    const u64 incl = block_scan<kPickWaves>(sum, s.waves, total);
+    const u64 incl = block_scan<kThreads / kWave>(sum, s.waves, total);
+    const u64 want = target_of(*total);
     u64 acc = incl - sum;
-    if (acc < target && incl >= target) {
+    if (acc < want && incl >= want) {
 #pragma unroll
         for (int i = 0; i < kPer; i++) {
-            if (acc < target && acc + v[i] >= target) {
+            if (acc < want && acc + v[i] >= want) {
                 s.found = kPer * tid + i;
                 s.found_base = acc;
             }
@@ -363,6 +416,7 @@ __device__ __forceinline__ int first_reaching(PickLds &s, int n, u64 target, u64
     __syncthreads();
     const int f = s.found;
     *base = f < n ? s.found_base : 0;
+    *target = want;
     __syncthreads();
     return f;
 }
@@ -385,18 +439,18 @@ __device__ __forceinline__ float bin_edge(double top_bin, int bin, double c) {
     return from_order_bits(k);
 }
 
-// Calls f(l, i) for every logit of the row (whole workgroup; a wavefront takes
-// runs of kRun consecutive ones, a lane four of them).
+// Calls f(run, l, i) for the logits of the row, l[0 .. 3] from index i (whole
+// workgroup; a wavefront takes runs of kRun consecutive ones, a lane four).
 template <typename T, typename F>
 __device__ __forceinline__ void for_row(const T *row, int V, F f) {
     const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
     const int runs = (V + kRun - 1) / kRun;
-    constexpr int kAhead = 4;
-    for (int r0 = wave; r0 < runs; r0 += kAhead * kPickWaves) {
+    constexpr int kAhead = 4, kWaves = kFilterThreads / kWave;
+    for (int r0 = wave; r0 < runs; r0 += kAhead * kWaves) {
         float l[kAhead][4];
 #pragma unroll
         for (int i = 0; i < kAhead; i++) {
-            const int at = (r0 + i * kPickWaves) * kRun + 4 * lane;
+            const int at = (r0 + i * kWaves) * kRun + 4 * lane;
             if (at + 4 <= V) {
                 if constexpr (sizeof(T) == 4) {
                     const f4_any v = *reinterpret_cast<const f4_any *>(row + at);
@@ -417,251 +471,63 @@ __device__ __forceinline__ void for_row(const T *row, int V, F f) {
         }
 #pragma unroll
         for (int i = 0; i < kAhead; i++)
-            if (r0 + i * kPickWaves < runs)
-                f(r0 + i * kPickWaves, l[i], (r0 + i * kPickWaves) * kRun + 4 * lane);
+            if (r0 + i * kWaves < runs)
+                f(r0 + i * kWaves, l[i], (r0 + i * kWaves) * kRun + 4 * lane);
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleParams a) {
-    extern __shared__ u64 pick_lds[];
-    PickLds &s = *reinterpret_cast<PickLds *>(pick_lds);
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
-    const RowRule rule = row_rule(a, b);
-    const size_t slice0 = (size_t)b * a.slices;
-    const T *row = static_cast<const T *>(a.logits) + (int64_t)b * a.row_stride;
+__device__ __forceinline__ float clamp_u(float u) { return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f; }
 
-    float m = -INFINITY;
-    for (int i = tid; i < a.slices; i += kPickThreads)
-        m = fmaxf(m, a.s_max[slice0 + i]);
-    m = block_max<kPickWaves>(m, s.red);
-    if (!(m > -INFINITY)) {   // nothing to draw from
-        if (tid == 0) {
-            a.token[b] = -1;
-            if (a.logprob)
-                a.logprob[b] = -INFINITY;
-        }
-        return;
-    }
-    if (rule.greedy) {
-        if (tid == 0)
-            s.found = INT_MAX;
-        __syncthreads();
-        for (int i = tid; i < a.slices; i += kPickThreads)
-            if (a.s_max[slice0 + i] == m)
-                atomicMin(&s.found, a.s_arg[slice0 + i]);
-        __syncthreads();
-        if (tid == 0) {
-            a.token[b] = s.found;
-            if (a.logprob)
-                a.logprob[b] = 0.0f;
-        }
-        return;
-    }
+// The running mass that the drawn token is the first to reach.
+__device__ __forceinline__ u64 draw_target(float u, u64 total) {
+    u64 lo, up;
+    fraction_of(u, total, &lo, &up);
+    return lo + 1;
+}
+// The running mass that the last token of a top-p is the first to reach.
+__device__ __forceinline__ u64 p_target(const RowRule &rule, u64 total) {
+    u64 lo, up;
+    fraction_of(fmaxf(rule.p, 0.0f), total, &lo, &up);
+    return up > 0 ? up : 1;
+}
 
-    const double c = rule.c, top = scaled(m, c), E = rint(top);
-    const float u = a.u[b] > 0.0f ? fminf(a.u[b], 0x1.fffffep-1f) : 0.0f;
-    u64 Z = 0, base = 0, unused, target;
-    int run, run_len;
-    double run_E = E;         // the unit of the weights inside the chosen run
-    u64 cut = 0;              // lowest rank that is kept
-    float low = -FLT_MAX;     // no logit below it is kept
-    const double min_x = rule.by_min ? log2((double)rule.min_p) : 0.0;
-    const auto passes_min = [&](float l) { return !rule.by_min || ((double)l - (double)m) * c >= min_x; };
+// min-p is w >= min_p on the logits' exact distance from the largest, m.
+__device__ __forceinline__ bool passes_min(const RowRule &rule, float l, float m) {
+    return !rule.by_min || ((double)l - (double)m) * rule.c >= rule.min_x;
+}
+// A logit below which nothing passes: one float32 below where min-p ends,
+// whichever way that rounds.
+__device__ __forceinline__ float min_p_edge(const RowRule &rule, float m) {
+    const double at = (double)m + rule.min_x / rule.c;
+    return at > -(double)FLT_MAX ? from_order_bits(order_bits((float)at + 0.0f) - 1) : -FLT_MAX;
+}
 
-    if (!rule.by_k && !rule.by_p && !rule.by_min) {
-        // the slices' masses in the row's unit
-        for (int i = tid; i < a.slices; i += kPickThreads) {
-            const float sm = a.s_max[slice0 + i];
-            const double d = sm > -INFINITY ? E - rint(scaled(sm, c)) : 64.0;
-            s.run[i] = d < 64.0 ? a.s_mass[slice0 + i] >> (int)d : 0;
-        }
-        __syncthreads();
-        run_len = a.slice_len;
-        run = first_reaching<1>(s, a.slices, 1, &base, &Z, [&](int i) { return s.run[i]; });
-        fraction_of(u, Z, &target, &unused);
-        run = first_reaching<1>(s, a.slices, target + 1, &base, &Z, [&](int i) { return s.run[i]; });
-        run = min(run, a.slices - 1);
-        run_E = rint(scaled(a.s_max[slice0 + run], c));
-        target = (target - base) << (int)(E - run_E);
-    } else {
-        bool listed = false;
-        if (rule.by_k || rule.by_p) {
-            // the slices' bins on the row's grid
-            for (int i = tid; i < kBins; i += kPickThreads) {
-                s.bin_count[i] = 0;
-                s.bin_mass[i] = 0;
-            }
-            __syncthreads();
-            const double top_bin = floor(top * kBinsPerOctave);
-            for (int i = tid; i < a.slices * kBins; i += kPickThreads) {
-                const float sm = a.s_max[slice0 + i / kBins];
-                const uint32_t n = a.h_count[slice0 * kBins + i];
-                if (n == 0)
-                    continue;
-                const double stop = scaled(sm, c);
-                const double off = top_bin - floor(stop * kBinsPerOctave), d = E - rint(stop);
-                const int bin = (int)fmin(off + i % kBins, (double)(kBins - 1));
-                atomicAdd(&s.bin_count[bin], n);
-                if (rule.by_p && d < 64.0)
-                    atomicAdd(&s.bin_mass[bin], a.h_mass[slice0 * kBins + i] >> (int)d);
-            }
-            __syncthreads();
+// A row whose maximum is known.
+struct Row {
+    int b;
+    float m;          // largest logit
+    double c, E;      // log2(e) / T; weights are in units of 2^(E - 42)
+    float u;
+};
 
-            // the bin in which a running sum reaches a target: the filter's last one
-            u64 above = 0, all = 0;
-            u64 want = rule.k;
-            bool by_count = rule.by_k;
-            int bin = kBins;
-            if (rule.by_k)
-                bin = first_reaching<1>(s, kBins, want, &above, &all, [&](int i) { return (u64)s.bin_count[i]; });
-            if (bin == kBins) {   // top-k off, or no fewer than the row has
-                by_count = false;
-                if (rule.by_p) {
-                    first_reaching<1>(s, kBins, 1, &above, &all, [&](int i) { return s.bin_mass[i]; });
-                    fraction_of(fmaxf(rule.p, 0.0f), all, &unused, &want);
-                    want = want > 0 ? want : 1;
-                    bin = first_reaching<1>(s, kBins, want, &above, &all, [&](int i) { return s.bin_mass[i]; });
-                    bin = min(bin, kBins - 1);
-                }
-            }
-            const bool then_p = by_count && rule.by_p;
-            if (bin < kBins) {
-                u64 n;
-                first_reaching<1>(s, bin + 1, ~0ull, &base, &n, [&](int i) { return (u64)s.bin_count[i]; });
-                listed = n <= kList;
-                low = bin_edge(top_bin, bin, c);
-                // in front of what a descent looks at: everything above the
-                // bin, unless the list (or a top-p after a top-k) holds that too
-                const bool whole = listed || then_p;
-                const float high = whole || bin == 0 ? INFINITY : bin_edge(top_bin, bin - 1, c);
-                if (!whole)
-                    want -= above;
-                if (tid == 0)
-                    s.n = 0;
-                __syncthreads();
-                if (listed) {
-                    for_row(row, a.V, [&](int, const float(&l)[4], int at) {
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (l[e] >= low) {
-                                const int i = atomicAdd(&s.n, 1);
-                                if (i < kList)   // (the bins counted no more)
-                                    s.list[i] = rank_of(l[e], at + e);
-                            }
-                    });
-                    __syncthreads();
-                }
-                const int n_list = min(s.n, kList);
-                // Runs f(rank, logit) over the list, or over the row's logits in [low, high).
-                const auto for_candidates = [&](auto f) {
-                    if (listed) {
-                        for (int i = tid; i < n_list; i += kPickThreads)
-                            f(s.list[i], from_order_bits((uint32_t)(s.list[i] >> kMaxVocabBits)));
-                    } else {
-                        for_row(row, a.V, [&](int, const float(&l)[4], int at) {
-#pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                if (l[e] >= low && l[e] < high)
-                                    f(rank_of(l[e], at + e), l[e]);
-                        });
-                    }
-                };
-                // The rank at which the running sum (of counts, or of weights) reaches `want`.
-                const auto descend = [&](bool counts, u64 want) {
-                    u64 prefix = 0;
-                    for (int shift = 32 + kMaxVocabBits; shift > 0;) {
-                        const int next = max(shift - kDigitBits, 0), digits = 1 << (shift - next);
-                        for (int i = tid; i < kDigits; i += kPickThreads)
-                            s.digit[i] = 0;
-                        __syncthreads();
-                        for_candidates([&](u64 rank, float l) {
-                            if (shift == 32 + kMaxVocabBits || rank >> shift == prefix)
-                                atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))],
-                                          counts ? 1ull : weight(scaled(l, c), E));
-                        });
-                        __syncthreads();
-                        u64 in_front, sum;
-                        int d = first_reaching<kDigits / kPickThreads>(s, digits, want, &in_front, &sum,
-                                                                       [&](int i) { return s.digit[i]; });
-                        if (d == digits) {   // short by rounding of the bins' masses: the last one
-                            want = sum;
-                            d = first_reaching<kDigits / kPickThreads>(s, digits, want, &in_front, &sum,
-                                                                       [&](int i) { return s.digit[i]; });
-                            d = min(d, digits - 1);
-                        }
-                        want -= in_front;
-                        prefix = prefix << (shift - next) | (u64)(digits - 1 - d);
-                        shift = next;
-                    }
-                    return prefix;
-                };
-                cut = descend(by_count, want);
-                if (then_p) {
-                    u64 kept = 0;
-                    for_candidates([&](u64 rank, float l) { kept += rank >= cut ? weight(scaled(l, c), E) : 0; });
-                    block_scan<kPickWaves>(kept, s.waves, &all);
-                    fraction_of(fmaxf(rule.p, 0.0f), all, &unused, &want);
-                    const u64 cut_p = descend(false, want > 0 ? want : 1);
-                    cut = cut_p > cut ? cut_p : cut;
-                }
-            }
-        }
-        // the kept mass of every run
-        const int runs = (a.V + kRun - 1) / kRun;
-        run_len = kRun;
-        if (listed) {
-            for (int i = tid; i < runs; i += kPickThreads)
-                s.run[i] = 0;
-            __syncthreads();
-            const int n_list = min(s.n, kList);
-            for (int i = tid; i < n_list; i += kPickThreads) {
-                const u64 rank = s.list[i];
-                const float l = from_order_bits((uint32_t)(rank >> kMaxVocabBits));
-                if (rank >= cut && passes_min(l))
-                    atomicAdd(&s.run[((1 << kMaxVocabBits) - 1 - (int)(rank & ((1 << kMaxVocabBits) - 1))) / kRun],
-                              weight(scaled(l, c), E));
-            }
-        } else {
-            if (cut)
-                low = fmaxf(low, from_order_bits((uint32_t)(cut >> kMaxVocabBits)));
-            if (rule.by_min) {   // one float32 below where min-p ends, whichever way that rounds
-                const double at = (double)m + min_x / c;
-                if (at > -(double)FLT_MAX)
-                    low = fmaxf(low, from_order_bits(order_bits((float)at + 0.0f) - 1));
-            }
-            for_row(row, a.V, [&](int r, const float(&l)[4], int at) {
-                u64 sum = 0;
-                if (__any(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= low)) {
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (l[e] >= low && rank_of(l[e], at + e) >= cut && passes_min(l[e]))
-                            sum += weight(scaled(l[e], c), E);
-                    sum = wave_incl_scan((uint64_t)sum);
-                }
-                if (lane == kWave - 1)
-                    s.run[r] = sum;
-            });
-        }
-        __syncthreads();
-        run = first_reaching<kMaxRuns / kPickThreads>(s, runs, 1, &base, &Z, [&](int i) { return s.run[i]; });
-        fraction_of(u, Z, &target, &unused);
-        run = first_reaching<kMaxRuns / kPickThreads>(s, runs, target + 1, &base, &Z, [&](int i) { return s.run[i]; });
-        run = min(run, runs - 1);
-        target -= base;
-    }
+__device__ __forceinline__ void write_token(const SampleParams &a, const Row &r, int token, float l, u64 Z) {
+    a.token[r.b] = token;
+    if (a.logprob)
+        a.logprob[r.b] = token < 0 ? -INFINITY : (float)((scaled(l, r.c) - r.E) * kLn2 - log((double)Z * 0x1p-42));
+}
 
-    // the token inside the run: the first whose running weight exceeds the target
-    const int per = (run_len + kPickThreads - 1) / kPickThreads;
-    const int at = run * run_len + tid * per, end = min(min(at + per, (run + 1) * run_len), a.V);
-    const auto kept_weight = [&](int i) -> u64 {
-        const float l = one_logit(row, i);
-        return l > -INFINITY && rank_of(l, i) >= cut && passes_min(l) ? weight(scaled(l, c), run_E) : 0;
-    };
+// The token inside a run of `len` logits from `first`: the first whose running
+// weight exceeds `target`; weights (get) are in the run's own unit.
+template <int kThreads, typename T, typename Get>
+__device__ __forceinline__ void draw_inside(const SampleParams &a, const Row &r, const T *row, DrawLds &s, int first, int len,
+                                            u64 target, u64 Z, Get get) {
+    const int tid = threadIdx.x;
+    const int per = (len + kThreads - 1) / kThreads;
+    const int at = first + tid * per, end = min(min(at + per, first + len), a.V);
     u64 sum = 0;
     int last = -1;
     for (int i = at; i < end; i++) {
-        const u64 w = kept_weight(i);
+        const u64 w = get(i);
         sum += w;
         last = w ? i : last;
     }
@@ -670,14 +536,14 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleParams 
         s.last = -1;
     }
     u64 total;
-    const u64 incl = block_scan<kPickWaves>(sum, s.waves, &total);
-    if (last >= 0)
-        atomicMax(&s.last, last);   // what rounding of a slice's shift may leave as the answer
+    const u64 incl = block_scan<kThreads / kWave>(sum, s.waves, &total);
+    if (total <= target && last >= 0)
+        atomicMax(&s.last, last);   // a run's shifted mass was a unit more than its weights
     u64 acc = incl - sum;
     if (acc <= target && incl > target) {
         int i = at;
         for (; i < end; i++) {
-            acc += kept_weight(i);
+            acc += get(i);
             if (acc > target)
                 break;
         }
@@ -686,16 +552,360 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleParams 
     __syncthreads();
     if (tid == 0) {
         const int token = s.found < a.V ? s.found : s.last;
-        a.token[b] = token;
-        if (a.logprob)
-            a.logprob[b] = token < 0 ? -INFINITY
-                                     : (float)((scaled(one_logit(row, token), c) - E) * kLn2 - log((double)Z * 0x1p-42));
+        write_token(a, r, token, token < 0 ? 0.0f : one_logit(row, token), Z);
     }
+}
+
+// Rows that need no filter: the largest logit, or the draw by the slices'
+// masses.  Returns whether the row was such a one.
+template <int kThreads, typename T>
+__device__ __forceinline__ bool draw_unfiltered(const SampleParams &a, const RowRule &rule, Row &r, const T *row, DrawLds &s) {
+    const int tid = threadIdx.x;
+    const size_t slice0 = (size_t)r.b * a.slices;
+    static_assert(kMaxSlices <= kPlanThreads, "one slice per thread");
+    const float sm = tid < a.slices ? a.s_max[slice0 + tid] : -INFINITY;
+    const u64 mass = tid < a.slices ? a.s_mass[slice0 + tid] : 0;   // (of a greedy or filtered row: not used)
+    r.u = clamp_u(a.u[r.b]);
+    r.m = block_max<kThreads / kWave>(sm, s.red);
+    r.c = rule.c;
+    if (!(r.m > -INFINITY)) {   // nothing to draw from
+        if (tid == 0)
+            write_token(a, r, -1, 0.0f, 0);
+        return true;
+    }
+    if (rule.greedy) {
+        if (tid == 0)
+            s.found = INT_MAX;
+        __syncthreads();
+        if (sm == r.m)
+            atomicMin(&s.found, a.s_arg[slice0 + tid]);
+        __syncthreads();
+        if (tid == 0) {
+            a.token[r.b] = s.found;
+            if (a.logprob)
+                a.logprob[r.b] = 0.0f;
+        }
+        return true;
+    }
+    r.E = rint(scaled(r.m, r.c));
+    if (rule.by_k || rule.by_p || rule.by_min)
+        return false;
+    // the slices' masses in the row's unit
+    const double d = sm > -INFINITY ? r.E - rint(scaled(sm, r.c)) : 64.0;
+    const u64 shifted = d < 64.0 ? mass >> (int)d : 0;
+    u64 base, Z, target;
+    int slice = first_reaching<kThreads, 1>(s, a.slices, &base, &Z, &target, [&](int) { return shifted; },
+                                              [&](u64 total) { return draw_target(r.u, total); });
+    slice = min(slice, a.slices - 1);
+    const double run_E = rint(scaled(a.s_max[slice0 + slice], r.c));
+    draw_inside<kThreads>(a, r, row, s, slice * a.slice_len, a.slice_len, (target - 1 - base) << (int)(r.E - run_E), Z,
+                          [&](int i) -> u64 {
+                              return weight(scaled(one_logit(row, i), r.c), run_E);
+                          });
+    return true;
+}
+
+// Draws the rows that need no filter, and finds out where the others' filters
+// end: the logits from `hi` on are kept by them, those in [lo, hi) are the
+// candidates among which a filter ends.
+template <typename T>
+__global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams a) {
+    __shared__ PlanLds s;
+    const int tid = threadIdx.x;
+    Row r;
+    r.b = blockIdx.x;
+    const RowRule rule = row_rule(a, r.b);
+    RowPlan plan;
+    plan.state = kDrawn;
+    if (draw_unfiltered<kPlanThreads>(a, rule, r, static_cast<const T *>(a.logits) + (int64_t)r.b * a.row_stride, s)) {
+        if (tid == 0)
+            a.plan[r.b] = plan;
+        return;
+    }
+    static_assert(kBins == kPlanThreads, "one bin per thread");
+    const double c = r.c, top = scaled(r.m, c);
+    plan.state = kListed;
+    plan.m = r.m;
+    plan.lo = plan.hi = -FLT_MAX;
+    plan.want = 0;
+    plan.by_count = plan.then_p = false;
+    plan.n = 0;
+    if (rule.by_min)
+        plan.lo = plan.hi = min_p_edge(rule, r.m);
+    if (rule.by_k || rule.by_p) {
+        // the slices' bins on the row's grid
+        s.bin_count[tid] = 0;
+        s.bin_mass[tid] = 0;
+        __syncthreads();
+        const size_t slice0 = (size_t)r.b * a.slices;
+        const double top_bin = floor(top * kBinsPerOctave);
+        for (int i = 0; i < a.slices; i++) {
+            const uint32_t n = a.h_count[(slice0 + i) * kBins + tid];
+            const u64 mass = rule.by_p ? a.h_mass[(slice0 + i) * kBins + tid] : 0;
+            if (n == 0)
+                continue;
+            const double stop = scaled(a.s_max[slice0 + i], c);
+            const double off = top_bin - floor(stop * kBinsPerOctave), d = r.E - rint(stop);
+            const int at = (int)fmin(off + tid, (double)(kBins - 1));
+            atomicAdd(&s.bin_count[at], n);
+            if (d < 64.0)
+                atomicAdd(&s.bin_mass[at], mass >> (int)d);
+        }
+        __syncthreads();
+        const u64 count = s.bin_count[tid];
+        u64 above, all, want, n_low, unused;
+        int bin = kBins;   // the bin in which the first filter ends
+        if (rule.by_k) {
+            bin = first_reaching<kPlanThreads, 1>(s, kBins, &above, &all, &want, [&](int) { return count; },
+                                                  [&](u64) { return (u64)rule.k; });
+            plan.by_count = bin < kBins;   // else the row has no more usable logits than k
+        }
+        if (!plan.by_count && rule.by_p)
+            bin = min(first_reaching<kPlanThreads, 1>(s, kBins, &above, &all, &want, [&](int i) { return s.bin_mass[i]; },
+                                                      [&](u64 total) { return p_target(rule, total); }),
+                      kBins - 1);
+        if (bin < kBins) {
+            plan.then_p = plan.by_count && rule.by_p;
+            first_reaching<kPlanThreads, 1>(s, bin + 1, &unused, &n_low, &unused, [&](int) { return count; }, [](u64) { return ~0ull; });
+            plan.lo = bin_edge(top_bin, bin, c);
+            plan.hi = INFINITY;
+            plan.want = want;
+            if (n_low > kList) {
+                if (!plan.then_p) {
+                    plan.hi = bin > 0 ? bin_edge(top_bin, bin - 1, c) : INFINITY;
+                    plan.want = want - above;
+                }
+                plan.state = !plan.then_p && s.bin_count[bin] <= kList ? kListed : kScanned;
+            }
+        }
+    }
+    if (tid == 0)
+        a.plan[r.b] = plan;
+}
+
+// Spreads the filtered rows over the chip a second time: appends each row's
+// candidates to its list and sums the weights of what is kept anyway.
+template <typename T, int kPasses>
+__global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SampleParams a) {
+    constexpr int kVec = 16 / sizeof(T), kLoads = 16 * kPasses / kVec;
+    __shared__ u64 waves[kSliceThreads / kWave];
+    __shared__ int at_list;
+    const int b = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const int tid = threadIdx.x;
+    const RowPlan &plan = a.plan[b];
+    if (plan.state != kListed)
+        return;
+    const float lo = plan.lo, hi = plan.hi, m = plan.m;
+    const size_t at_slice = (size_t)b * a.slices + slice;
+    if (a.s_max[at_slice] < lo) {   // nothing here
+        if (tid == 0)
+            a.s_mass[at_slice] = 0;
+        return;
+    }
+    const RowRule rule = row_rule(a, b);
+    const int first = slice * a.slice_len, n = min(a.V - first, a.slice_len);
+    const T *src = static_cast<const T *>(a.logits) + (int64_t)b * a.row_stride + first;
+    float l[kLoads][kVec];
+    load_slice<T, kPasses>(src, n, l);
+    const double E = rint(scaled(m, rule.c));
+    u64 sum = 0;
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; i++)
+#pragma unroll
+        for (int e = 0; e < kVec; e++) {
+            mine += l[i][e] >= lo && l[i][e] < hi;
+            if (__any(l[i][e] >= hi))
+                sum += l[i][e] >= hi && passes_min(rule, l[i][e], m) ? weight(scaled(l[i][e], rule.c), E) : 0;
+        }
+    u64 total;
+    block_scan<kSliceThreads / kWave>(sum, waves, &total);
+    if (tid == 0)
+        a.s_mass[at_slice] = total;
+    u64 all;
+    int at = (int)block_scan<kSliceThreads / kWave>((u64)mine, waves, &all) - mine;
+    if (all == 0)
+        return;
+    if (tid == 0)
+        at_list = atomicAdd(&a.plan[b].n, (int)all);
+    __syncthreads();
+    at += at_list;
+#pragma unroll
+    for (int i = 0; i < kLoads; i++)
+#pragma unroll
+        for (int e = 0; e < kVec; e++)
+            if (l[i][e] >= lo && l[i][e] < hi) {
+                if (at < a.list_len)   // (the bins counted no more)
+                    a.list[(size_t)b * a.list_len + at] = rank_of(l[i][e], first + (i * kSliceThreads + tid) * kVec + e);
+                at++;
+            }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SampleParams a) {
+    extern __shared__ u64 pick_lds[];
+    FilterLds &s = *reinterpret_cast<FilterLds *>(pick_lds);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    Row r;
+    r.b = blockIdx.x;
+    const RowPlan plan = a.plan[r.b];
+    if (plan.state == kDrawn)
+        return;
+    const RowRule rule = row_rule(a, r.b);
+    const size_t slice0 = (size_t)r.b * a.slices;
+    const T *row = static_cast<const T *>(a.logits) + (int64_t)r.b * a.row_stride;
+    r.u = clamp_u(a.u[r.b]);
+    r.m = plan.m;
+    r.c = rule.c;
+    r.E = rint(scaled(r.m, r.c));
+    const bool listed = plan.state == kListed;
+    const int n_list = listed ? min(plan.n, a.list_len) : 0;
+    for (int i = tid; i < n_list; i += kFilterThreads)
+        s.list[i] = a.list[(size_t)r.b * a.list_len + i];
+    if (tid < a.slices)
+        s.slice[tid] = listed ? a.s_mass[slice0 + tid] : 0;
+    __syncthreads();
+
+    const auto weight_of = [&](float l) { return weight(scaled(l, r.c), r.E); };
+    const auto logit_of = [](u64 rank) { return from_order_bits((uint32_t)(rank >> kMaxVocabBits)); };
+    constexpr int kIndex = (1 << kMaxVocabBits) - 1;
+    const auto index_of = [](u64 rank) { return kIndex - (int)(rank & kIndex); };
+    u64 all;
+
+    if (listed && plan.hi == INFINITY && n_list <= kFew) {
+        // Few logits in question: each thread compares its own with all the others.
+        u64 *w_of = s.digit;
+        const bool mine = tid < n_list;
+        const u64 rank = mine ? s.list[tid] : 0, w = mine ? weight_of(logit_of(rank)) : 0;
+        if (mine)
+            w_of[tid] = w;
+        __syncthreads();
+        u64 in_front = 0, mass_in_front = 0;
+        if (mine)
+            for (int j = 0; j < n_list; j++) {
+                const bool first = s.list[j] > rank;
+                in_front += first;
+                mass_in_front += first ? w_of[j] : 0;
+            }
+        bool kept = mine && !(plan.by_count && in_front >= (u64)rule.k);
+        if (rule.by_p) {
+            u64 want = plan.want;   // without top-k, of the whole row's mass
+            if (plan.by_count) {
+                block_scan<kFilterThreads / kWave>(kept ? w : 0, s.waves, &all);
+                want = p_target(rule, all);
+            }
+            kept = kept && mass_in_front < want;
+        }
+        kept = kept && passes_min(rule, logit_of(rank), r.m);
+        u64 Z;
+        block_scan<kFilterThreads / kWave>(kept ? w : 0, s.waves, &Z);   // (its barriers order the loops' reads)
+        if (mine)
+            w_of[tid] = kept ? w : 0;
+        __syncthreads();
+        u64 target, unused, before = 0;
+        fraction_of(r.u, Z, &target, &unused);
+        if (kept)
+            for (int j = 0; j < n_list; j++)
+                before += index_of(s.list[j]) < index_of(rank) ? w_of[j] : 0;
+        if (kept && before <= target && target < before + w)
+            write_token(a, r, index_of(rank), logit_of(rank), Z);
+        return;
+    }
+
+    u64 cut = 0;   // lowest rank that is kept
+    if (plan.want) {
+        // Finds the rank at which the running sum (of counts, or of weights) of
+        // the candidates reaches `want`, from its highest digit down; for a
+        // top-p of what a top-k keeps, once more with the weights.  Candidates
+        // that do not fit a list are read from the row.
+        bool counts = plan.by_count;
+        u64 want = plan.want;
+        for (int round = 0; round <= (int)plan.then_p; round++) {
+            u64 prefix = 0;
+            const u64 floor_rank = cut;
+            u64 kept = 0;
+            for (int shift = 32 + kMaxVocabBits; shift >= 0;) {
+                // the last pass only sums the weights of what is kept
+                const bool summing = shift == 0;
+                if (summing && !(plan.then_p && round == 0))
+                    break;
+                const int next = max(shift - kDigitBits, 0), digits = 1 << (shift - next);
+                for (int i = tid; i < kDigits; i += kFilterThreads)
+                    s.digit[i] = 0;
+                __syncthreads();
+                const auto take = [&](u64 rank, float l) {
+                    if (summing)
+                        kept += rank >= prefix ? weight_of(l) : 0;
+                    else if ((shift == 32 + kMaxVocabBits || rank >> shift == prefix) && rank >= floor_rank)
+                        atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight_of(l));
+                };
+                if (listed) {
+                    for (int i = tid; i < n_list; i += kFilterThreads)
+                        take(s.list[i], logit_of(s.list[i]));
+                } else {
+                    for_row(row, a.V, [&](int, const float(&l)[4], int at) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (l[e] >= plan.lo && l[e] < plan.hi)
+                                take(rank_of(l[e], at + e), l[e]);
+                    });
+                }
+                if (summing)
+                    break;
+                __syncthreads();
+                u64 in_front, sum, goal;
+                // (a target past the sum, by rounding of the bins' masses, takes the last one)
+                int d = first_reaching<kFilterThreads, kDigits / kFilterThreads>(
+                    s, digits, &in_front, &sum, &goal, [&](int i) { return s.digit[i]; },
+                    [&](u64 sum) { return want < sum ? want : sum; });
+                d = min(d, digits - 1);
+                want = goal - in_front;
+                prefix = prefix << (shift - next) | (u64)(digits - 1 - d);
+                shift = next;
+            }
+            cut = prefix;
+            if (plan.then_p && round == 0) {
+                block_scan<kFilterThreads / kWave>(kept, s.waves, &all);
+                want = p_target(rule, all);
+                counts = false;
+            }
+        }
+    }
+
+    // the kept mass of every slice, and the draw
+    if (listed) {
+        for (int i = tid; i < n_list; i += kFilterThreads) {
+            const u64 rank = s.list[i];
+            const float l = logit_of(rank);
+            if (rank >= cut && passes_min(rule, l, r.m))
+                atomicAdd(&s.slice[index_of(rank) / a.slice_len], weight_of(l));
+        }
+    } else {
+        for_row(row, a.V, [&](int run, const float(&l)[4], int at) {
+            u64 sum = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (l[e] >= plan.lo && rank_of(l[e], at + e) >= cut && passes_min(rule, l[e], r.m))
+                    sum += weight_of(l[e]);
+            sum = wave_incl_scan((uint64_t)sum);
+            if (lane == kWave - 1 && sum)
+                atomicAdd(&s.slice[run * kRun / a.slice_len], sum);
+        });
+    }
+    __syncthreads();
+    u64 Z, target, base;
+    int slice = first_reaching<kFilterThreads, 1>(s, a.slices, &base, &Z, &target, [&](int i) { return s.slice[i]; },
+                                                  [&](u64 total) { return draw_target(r.u, total); });
+    slice = min(slice, a.slices - 1);
+    draw_inside<kFilterThreads>(a, r, row, s, slice * a.slice_len, a.slice_len, target - 1 - base, Z, [&](int i) -> u64 {
+        const float l = one_logit(row, i);
+        return l >= plan.lo && rank_of(l, i) >= cut && passes_min(rule, l, r.m) ? weight_of(l) : 0;
+    });
 }
 
 struct SamplePlan {
     int slices, slice_len;
-    size_t arg_off, mass_off, count_off, hmass_off, bytes;
+    size_t arg_off, mass_off, count_off, hmass_off, plan_off, list_off, bytes;
 };
 
 // Short slices spread few rows over the chip; from 2,048 workgroups on longer
@@ -714,18 +924,26 @@ int make_sample_plan(int32_t B, int32_t V, SamplePlan *pl) {
     pl->mass_off = pl->arg_off + up(n * sizeof(int32_t));
     pl->count_off = pl->mass_off + up(n * sizeof(u64));
     pl->hmass_off = pl->count_off + up(n * kBins * sizeof(uint32_t));
-    pl->bytes = pl->hmass_off + up(n * kBins * sizeof(u64));
+    pl->plan_off = pl->hmass_off + up(n * kBins * sizeof(u64));
+    pl->list_off = pl->plan_off + up(B * sizeof(RowPlan));
+    pl->bytes = pl->list_off + up((size_t)B * std::min(kList, V) * sizeof(u64));
     return TS_OK;
 }
 
-template <typename T>
+template <typename T, int kPasses>
 hipError_t launch_sample(const SampleParams &a, int B, hipStream_t hs) {
-    const auto slices = a.slice_len == kSliceUnit ? sample_slices_kernel<T, 1> : sample_slices_kernel<T, kLongSlice>;
-    hipLaunchKernelGGL(slices, dim3((unsigned)B * (unsigned)a.slices), dim3(kSliceThreads), 0, hs, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
+    const unsigned rows = (unsigned)B, slices = rows * (unsigned)a.slices;
+    hipError_t e;
+    hipLaunchKernelGGL((sample_slices_kernel<T, kPasses>), dim3(slices), dim3(kSliceThreads), 0, hs, a);
+    if ((e = hipGetLastError()) != hipSuccess)
         return e;
-    hipLaunchKernelGGL(sample_pick_kernel<T>, dim3((unsigned)B), dim3(kPickThreads), sizeof(PickLds), hs, a);
+    hipLaunchKernelGGL(sample_plan_kernel<T>, dim3(rows), dim3(kPlanThreads), 0, hs, a);
+    if ((e = hipGetLastError()) != hipSuccess || !(a.top_k || a.top_p || a.min_p))
+        return e;
+    hipLaunchKernelGGL((sample_gather_kernel<T, kPasses>), dim3(slices), dim3(kSliceThreads), 0, hs, a);
+    if ((e = hipGetLastError()) != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(sample_filter_kernel<T>, dim3(rows), dim3(kFilterThreads), sizeof(FilterLds), hs, a);
     return hipGetLastError();
 }
 
@@ -778,13 +996,18 @@ int ts_sample(int32_t num_seqs, int32_t vocab, int32_t logits_type, const void *
     a.s_mass = reinterpret_cast<u64 *>(ws + pl.mass_off);
     a.h_count = reinterpret_cast<uint32_t *>(ws + pl.count_off);
     a.h_mass = reinterpret_cast<u64 *>(ws + pl.hmass_off);
+    a.plan = reinterpret_cast<RowPlan *>(ws + pl.plan_off);
+    a.list = reinterpret_cast<u64 *>(ws + pl.list_off);
+    a.list_len = std::min(kList, vocab);
     a.row_stride = row_stride;
     a.V = vocab;
     a.slices = pl.slices;
     a.slice_len = pl.slice_len;
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
-    const hipError_t e = logits_type == TS_LOGITS_F32 ? launch_sample<float>(a, num_seqs, hs)
-                                                      : launch_sample<uint16_t>(a, num_seqs, hs);
+    const bool f32 = logits_type == TS_LOGITS_F32, shorter = pl.slice_len == kSliceUnit;
+    const hipError_t e = f32 ? (shorter ? launch_sample<float, 1>(a, num_seqs, hs) : launch_sample<float, kLongSlice>(a, num_seqs, hs))
+                             : (shorter ? launch_sample<uint16_t, 1>(a, num_seqs, hs)
+                                        : launch_sample<uint16_t, kLongSlice>(a, num_seqs, hs));
     return e == hipSuccess ? TS_OK : hip_fail(e, "sampling launch");
 }
 
