@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "chunk_common.h"
@@ -18,7 +19,8 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRowBlock = 32;      // rows of a matrix-core tile
-constexpr int kChunkWaves = 4;
+constexpr int kChunkWaves = 8;
+constexpr int kStages = 4;         // KV tiles in LDS: one in use, the others on their way
 constexpr int kTileRows = kChunkWaves * kRowBlock;
 constexpr float kTiny = 1.17549435e-38f;   // the smallest normal float32
 constexpr int kTilePages = kKeyTile / kPage;
@@ -60,8 +62,8 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
     return s;
 }
 
-// Exclusive prefix over the sequences of one head's KV tiles, in s_pre[0..B].
-__device__ inline void tile_prefix(const ChunkParams &p, uint64_t *s_pre) {
+// KV tiles of one head up to the end of each sequence, in s_end[0 .. B - 1].
+__device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
     if (threadIdx.x < kWave) {
         const int lane = threadIdx.x;
         uint64_t base = 0;
@@ -74,11 +76,9 @@ __device__ inline void tile_prefix(const ChunkParams &p, uint64_t *s_pre) {
             }
             const uint64_t incl = wave_incl_scan(n);
             if (b < p.B)
-                s_pre[b] = base + incl - n;
+                s_end[b] = base + incl;
             base += __shfl(incl, kWave - 1, kWave);
         }
-        if (lane == 0)
-            s_pre[p.B] = base;
     }
     __syncthreads();
 }
@@ -92,22 +92,31 @@ struct Piece {
     int64_t next;
 };
 
+// Ends a piece of unit r.us, r.m that starts at tile j0: with the unit, or with the range.
+__device__ __forceinline__ void cut_piece(Piece &r, const ChunkSeq &c, int64_t range_end) {
+    r.n = c.cost(r.m);
+    const int64_t unit_end = r.us + r.n + kUnitTiles;
+    r.next = unit_end < range_end ? unit_end : range_end;
+    r.j1 = first_lane_int(min((int)(r.next - r.us), r.n));   // (not above j0 in the places without tiles)
+    r.whole = r.j0 == 0 && r.j1 == r.n;
+}
+
 // The unit that holds global tile x, and the part of it in [x, range_end).
 // Units are laid out sequence by sequence, head by head, row tile by row tile.
-__device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_pre, int64_t x, int64_t range_end) {
+__device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end, int64_t x, int64_t range_end) {
     const int lane = threadIdx.x & (kWave - 1);
     Piece r;
-    // the last sequence that starts at or before x
+    // the first sequence that ends behind x
     int lo = 0, n = p.B;
+    const auto before = [&](int b) { return (int64_t)s_end[min(b, p.B - 1)] * p.Hkv <= x; };
     if (p.B > kWave) {
-        const int step = (p.B + kWave - 1) / kWave;
-        const int at = lane * step;
-        lo = step * (__popcll(__ballot(at < p.B && (int64_t)s_pre[min(at, p.B)] * p.Hkv <= x)) - 1);
+        const int step = (p.B + kWave - 1) / kWave, last = (lane + 1) * step - 1;
+        lo = step * __popcll(__ballot(last < p.B && before(last)));
         n = min(step, p.B - lo);
     }
-    r.b = first_lane_int(lo + __popcll(__ballot(lane < n && (int64_t)s_pre[min(lo + lane, p.B)] * p.Hkv <= x)) - 1);
-    const int64_t pre = first_lane_int64((int64_t)s_pre[r.b]);
-    const int64_t per_head = first_lane_int64((int64_t)s_pre[r.b + 1]) - pre;
+    r.b = first_lane_int(min(lo + __popcll(__ballot(lane < n && before(lo + lane))), p.B - 1));
+    const int64_t pre = r.b ? first_lane_int64((int64_t)s_end[r.b - 1]) : 0;
+    const int64_t per_head = first_lane_int64((int64_t)s_end[r.b]) - pre;
     const int64_t off = x - pre * p.Hkv;
     r.g = first_lane_int((int)(off / per_head));
     const int64_t in_head = off - r.g * per_head;
@@ -125,14 +134,34 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_pre,
     }
     r.m = first_lane_int(m);
     const int64_t start = c.before(r.m);
-    r.n = c.cost(r.m);
     r.us = x - in_head + start;
     r.j0 = first_lane_int((int)(in_head - start));
-    const int64_t unit_end = r.us + r.n;
-    r.next = unit_end < range_end ? unit_end : range_end;
-    r.j1 = first_lane_int((int)(r.next - r.us));
-    r.whole = r.j0 == 0 && r.j1 == r.n;
+    cut_piece(r, c, range_end);
     return r;
+}
+
+// The next piece with KV tiles at or behind x in a worker's range, false if
+// there is none.  `r` is the piece before it, if `started`: the row tiles of one
+// head follow each other, so most of the time nothing is searched.
+__device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t *s_end, int64_t &x, int64_t range_end, bool started, Piece &r) {
+    while (x < range_end) {
+        const ChunkSeq c = started ? seq_info(p, r.b).c : ChunkSeq{0, 0, 1};
+        if (started && (r.m + 1 < c.tiles() || r.g + 1 < p.Hkv)) {
+            const bool same = r.m + 1 < c.tiles();
+            r.g = same ? r.g : r.g + 1;
+            r.m = same ? r.m + 1 : 0;
+            r.j0 = 0;
+            r.us = x;
+            cut_piece(r, c, range_end);
+        } else {
+            r = locate_tile(p, s_end, x, range_end);
+        }
+        started = true;
+        x = r.next;
+        if (r.j0 < r.j1)
+            return true;
+    }
+    return false;
 }
 
 __device__ __forceinline__ float max_both_halves(float x) {
@@ -150,86 +179,237 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
+
+// Loads kLoads blocks of 1 KiB into LDS without passing registers: block i from
+// byte (from ^ (twist i)) + 1024 i of the resource (each lane 16 bytes), to `to`
+// + 1024 i + 16 lane.  The instructions have no outputs, so nothing can be taken
+// for written before it is; m0, which they need, has no other use in these
+// kernels.  Completion is counted by vmcnt: dma_wait() and a barrier come before
+// the data is read.
+template <int kLoads>
+__device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int from, int twist) {
+    static_assert(kLoads == 2 || kLoads == 4, "blocks");
+    if constexpr (kLoads == 4)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
+                     "buffer_load_dwordx4 %3, %1, 0 offen offset:1024 lds\n\t"
+                     "buffer_load_dwordx4 %4, %1, 0 offen offset:2048 lds\n\t"
+                     "buffer_load_dwordx4 %5, %1, 0 offen offset:3072 lds"
+                     ::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist), "v"(from ^ 2 * twist), "v"(from ^ 3 * twist)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
+                     "buffer_load_dwordx4 %3, %1, 0 offen offset:1024 lds"
+                     ::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist) : "memory");
+}
+// Waits until at most the loads of the last `later` tiles are under way.
+template <int kLoads>
+__device__ __forceinline__ void dma_wait(int later) {
+    static_assert(kStages == 4, "up to two later tiles");
+    if (later >= 2)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+    else if (later == 1)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
 template <int D>
 struct Chunk {
     static constexpr int kRowBytes = 2 * D;
     static constexpr int kPieces = kRowBytes / 16;         // 16-byte pieces of a row
-    static constexpr int kVPitch = kRowBytes + 32;
-    static constexpr int kKBytes = kKeyTile * kRowBytes;
-    static constexpr int kVBytes = kKeyTile * kVPitch;
-    static constexpr int kStage = kKBytes + kVBytes;
-    static constexpr int kLds = 2 * kStage;
+    static constexpr int kKBytes = kKeyTile * kRowBytes;   // the keys of a stage; the values follow
+    static constexpr int kStage = 2 * kKBytes;
+    static constexpr int kLds = kStages * kStage;
     static constexpr int kLoads = kPage * kRowBytes / (16 * kWave);   // loads of a wave per page block
     static constexpr int kKSteps = D / 16;
     static constexpr int kDTiles = D / 32;
 
-    struct Stage {
-        u32x4_t k[kLoads], v[kLoads];
-    };
-
-    // Wave w loads page w of KV tile j: rows at or past `L` and pages outside
-    // the pool read as zeros (buffer bounds), without a memory access.
-    __device__ __forceinline__ static void load_tile(const ChunkParams &p, const int32_t *pt, int g, int j, int L, int wave, int lane,
-                                     Stage &s) {
-        const int page = j * kTilePages + wave;
-        const int rows = min(max(L - page * kPage, 0), kPage);
-        const int pid = ld_meta(pt, rows > 0 ? page : 0);
-        const bool ok = rows > 0 && pid >= 0 && pid < p.num_pages;
-        const size_t base = ((size_t)(ok ? pid : 0) * p.Hkv + g) * (size_t)(kPage * D);
-        const int bytes = ok ? rows * kRowBytes : 0;
-        const block_rsrc_t rk = block_rsrc(p.k_pages + base, bytes);
-        const block_rsrc_t rv = block_rsrc(p.v_pages + base, bytes);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            s.k[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, 16 * (i * kWave + lane), 0, 0);
-            s.v[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, 16 * (i * kWave + lane), 0, 0);
-        }
-    }
-
-    __device__ __forceinline__ static int k_addr(int key, int piece) {
-        return key * kRowBytes + ((piece ^ (key & (kPieces - 1))) << 4);
-    }
-
-    // `clean`: infinite and NaN values are staged as zero; returns whether there were any.
-    __device__ __forceinline__ static bool store_tile(char *stage, int wave, int lane, Stage &s, bool clean) {
-        bool odd = false;
-        if (clean)
-#pragma unroll
-            for (int i = 0; i < kLoads; i++)
-                odd |= clear_odd(s.v[i]);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int at = i * kWave + lane;
-            const int key = kPage * wave + at / kPieces, piece = at % kPieces;
-            *reinterpret_cast<u32x4_t *>(stage + k_addr(key, piece)) = s.k[i];
-            *reinterpret_cast<u32x4_t *>(stage + kKBytes + key * kVPitch + 16 * piece) = s.v[i];
-        }
-        return odd;
-    }
+    // Row `key` of a tile is stored with its 16-byte pieces in an order that
+    // depends on the key, so that reads of one column of many rows spread over
+    // the 64 banks.  Keys: 32 lanes read a piece of a row each, 16 bytes, and
+    // the sixteen that are served together have sixteen different keys modulo
+    // 16.  Values: 32 lanes read 32 bytes of four consecutive rows, at two
+    // places.  (Rows of 128 bytes: two fill the banks once.)
+    __device__ __forceinline__ static int k_piece(int key, int piece) { return piece ^ (D == 128 ? key & 15 : key >> 1 & 7); }
+    __device__ __forceinline__ static int v_piece(int key, int piece) { return piece ^ (D == 128 ? 4 * (key & 3) : 4 * (key >> 1 & 1)); }
 
     struct State {
         u32x4_t qf[kKSteps];
         f32x16_t o[kDTiles];
         float m_ref, l;
-        int lim;      // keys that this lane's row sees
+        int lim;                  // keys that this lane's row sees
+        // this lane's LDS addresses in stage 0, of the first keys and values
+        uint32_t k, v;
+        int from, twist;          // and where in a page it loads from (dma_blocks)
     };
 
-    __device__ __forceinline__ static bf16x8_t v_frag(const char *v, int dt, int step, int lane) {
-        typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-        const int h = lane >> 5, i = lane & 15;
-        const char *at = v + (16 * step + 4 * h + (i >> 2)) * kVPitch + 2 * (32 * dt + 16 * ((lane >> 4) & 1) + 4 * (i & 3));
-        const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(__attribute__((address_space(3))) const char *)at);
-        const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4 *)(__attribute__((address_space(3))) const char *)(at + 8 * kVPitch));
-        s16x4_t ab[2] = {a, b};
+    // Starts loading a wavefront's part of a tile, the keys (wavefronts 0 to 3)
+    // or values of a page.  A page outside the pool is stored as zeros; what is
+    // under way then arrives first, so that counts of loads stay counts of tiles.
+    __device__ __forceinline__ static void dma_page(const ChunkParams &p, const State &st, int pid, int g, char *stage, int wave, int lane) {
+        char *to = stage + wave * (kPage * kRowBytes);   // (the values follow the keys)
+        if (__builtin_expect(pid < 0 || pid >= p.num_pages, 0)) {
+            dma_wait<kLoads>(0);
+#pragma unroll
+            for (int i = 0; i < kLoads; i++)
+                *reinterpret_cast<u32x4_t *>(to + 16 * (i * kWave + lane)) = u32x4_t{0u, 0u, 0u, 0u};
+            return;
+        }
+        const size_t base = ((size_t)pid * p.Hkv + g) * (size_t)(kPage * D);
+        const block_rsrc_t rsrc = block_rsrc((wave < kTilePages ? p.k_pages : p.v_pages) + base, kPage * kRowBytes);
+        dma_blocks<kLoads>(rsrc, first_lane_int((int)(uintptr_t)(lds_char *)to), st.from, st.twist);
+    }
+
+    __device__ __forceinline__ static void set_addresses(State &st, char *lds, int wave, int lane) {
+        const int n = lane & 31, h = lane >> 5;
+        const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)lds;
+        st.k = base + n * kRowBytes + 16 * k_piece(n, h);
+        // Value operand.  ds_read_b64_tr_b16 hands lane i of 16 lanes element
+        // i % 4 of the 8 bytes that lane 4 k + i / 4 addresses, as element k;
+        // so with lane i addressing key i / 4, dimensions 4 (i % 4) .. + 3 of
+        // 16, it receives four keys of dimension i.
+        const int i = lane & 15, x = i >> 2;
+        st.v = base + kKBytes + (4 * h + x) * kRowBytes + 16 * v_piece(x, 2 * ((lane >> 4) & 1)) + 8 * (i & 3);
+        // Block i of 1 KiB of a page holds its rows (64 / kPieces) i + lane /
+        // kPieces in stored order: the exchange of key pieces differs by 4 i,
+        // 64 i bytes, that of value pieces not at all.
+        const int row = lane / kPieces, piece = lane % kPieces;
+        const bool keys = wave < kTilePages;
+        st.from = row * kRowBytes + 16 * (keys ? k_piece(row, piece) : v_piece(row, piece));
+        st.twist = keys ? 64 : 0;
+    }
+
+    // Keys 32 kt .. + 31, dimensions 16 ks .. + 15.
+    __device__ __forceinline__ static bf16x8_t k_frag(const State &st, int stage, int kt, int ks) {
+        const lds_char *at = (const lds_char *)(uintptr_t)((st.k + stage) ^ (32 * ks));
+        return __builtin_bit_cast(bf16x8_t, *(const lds_u32x4 *)(at + 32 * kRowBytes * kt));
+    }
+    // Dimensions 32 dt .. + 31 of the 16 keys of a step, in the order in which
+    // a lane's score registers hold them: 4 h .. + 3 and 8 + 4 h .. + 3.
+    __device__ __forceinline__ static bf16x8_t v_frag(const State &st, int stage, int dt, int step) {
+        const lds_char *at = (const lds_char *)(uintptr_t)((st.v + stage) ^ (64 * dt)) + 16 * kRowBytes * step;
+        s16x4_t ab[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at),
+                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * kRowBytes))};
         return __builtin_bit_cast(bf16x8_t, ab);
+    }
+
+    __device__ __forceinline__ static float max16(const f32x16_t &s) {
+        float m = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int e = 2; e < 16; e += 2)
+            m = fmaxf(fmaxf(m, s[e]), s[e + 1]);
+        return m;
+    }
+
+    // Raises the reference where a score exceeds it by more than the slack;
+    // `pf`, if any, holds weights that were taken with the old one.
+    __device__ __forceinline__ static void raise(State &st, float mx, u32x4_t *pf) {
+        if (__builtin_expect(__any(mx > st.m_ref + kRescaleSlack), 0)) {
+            mx = max_both_halves(mx);
+            const bool up = mx > st.m_ref + kRescaleSlack;
+            // (never zero, so that an infinite sum stays infinite)
+            const float alpha = up ? fmaxf(fast_exp2(st.m_ref - mx), kTiny) : 1.0f;
+            st.m_ref = up ? mx : st.m_ref;
+            st.l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    st.o[dt][e] *= alpha;
+            if (pf)
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    pf[i / 4][i % 4] = pack_bf16x2(bf16_lo(pf[i / 4][i % 4]) * alpha, bf16_hi(pf[i / 4][i % 4]) * alpha);
+        }
+    }
+
+    // Weights of 32 keys, packed in the order of the value operand.
+    template <bool kMasked>
+    __device__ __forceinline__ static void weights(const ChunkParams &p, State &st, f32x16_t &s, int room, u32x4_t (&pf)[2]) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+            float x = fast_exp2(__builtin_fmaf(s[e], p.scale_log2, -st.m_ref));
+            if constexpr (kMasked)
+                x = 8 * (e / 4) + e % 4 < room ? x : 0.0f;
+            s[e] = x;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+            sum += s[e];
+        st.l += sum;
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            pf[e / 4][e % 4] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
+    }
+
+    template <bool kMasked>
+    __device__ __forceinline__ static void mask(f32x16_t &s, int room) {
+        if constexpr (kMasked)
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+                s[e] = 8 * (e / 4) + e % 4 < room ? s[e] : -INFINITY;
+    }
+
+    // One KV tile.  The two halves of 32 keys overlap: the second half's score
+    // products run while the first half's weights are taken, the first half's
+    // value products while the second's are.
+    // `stage` is its byte offset; masked, the key of a lane's register e of half
+    // kt is seen if 32 kt + 8 (e / 4) + e % 4 is below `room`.
+    template <bool kMasked>
+    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, int stage, int room) {
+        const f32x16_t zero = {};
+        f32x16_t s0 = zero, s1 = zero;
+        bf16x8_t a[kKSteps], c[kKSteps];
+#pragma unroll
+        for (int ks = 0; ks < kKSteps; ks++)
+            a[ks] = k_frag(st, stage, 0, ks);
+#pragma unroll
+        for (int ks = 0; ks < kKSteps; ks++) {
+            s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], __builtin_bit_cast(bf16x8_t, st.qf[ks]), s0, 0, 0, 0);
+            c[ks] = k_frag(st, stage, 1, ks);
+        }
+        mask<kMasked>(s0, room);
+        raise(st, max16(s0) * p.scale_log2, nullptr);
+        u32x4_t p0[2], p1[2];
+        bf16x8_t v0[2][kDTiles];
+#pragma unroll
+        for (int ks = 0; ks < kKSteps; ks++)
+            s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[ks], __builtin_bit_cast(bf16x8_t, st.qf[ks]), s1, 0, 0, 0);
+        weights<kMasked>(p, st, s0, room, p0);
+#pragma unroll
+        for (int step = 0; step < 2; step++)
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+                v0[step][dt] = v_frag(st, stage, dt, step);
+        mask<kMasked>(s1, room - 32);
+        raise(st, max16(s1) * p.scale_log2, p0);
+        bf16x8_t v1[2][kDTiles];
+#pragma unroll
+        for (int step = 0; step < 2; step++)
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++) {
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[step][dt], __builtin_bit_cast(bf16x8_t, p0[step]), st.o[dt], 0, 0, 0);
+                v1[step][dt] = v_frag(st, stage, dt, 2 + step);
+            }
+        weights<kMasked>(p, st, s1, room - 32, p1);
+#pragma unroll
+        for (int step = 0; step < 2; step++)
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[step][dt], __builtin_bit_cast(bf16x8_t, p1[step]), st.o[dt], 0, 0, 0);
     }
 
     // Infinite and NaN values.  Where a row does not see a key, the key's zero
     // weight would still make NaN of such a value in the matrix product.  So in
     // the tiles that some row of the unit does not see whole (the last one to
-    // three) they are replaced by zero when the tile is staged, and put back
-    // afterwards for the rows that see them, whose result is infinite or NaN
+    // three) they are replaced by zero in LDS before the tile is used, and put
+    // back afterwards for the rows that see them, whose result is infinite or NaN
     // whatever the weight.
     static __device__ __forceinline__ bool clear_odd(u32x4_t &v) {
         bool odd = false;
@@ -241,6 +421,23 @@ struct Chunk {
             v[i] = hi ? v[i] & 0x0000ffffu : v[i];
         }
         return odd;
+    }
+
+    // The values of the page that this wavefront has loaded; returns whether one
+    // of its first `rows` rows held such a value (the others are not in the context).
+    __device__ __forceinline__ static bool clean_page(char *stage, int wave, int lane, int rows) {
+        char *page = stage + wave * (kPage * kRowBytes);
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            u32x4_t *at = reinterpret_cast<u32x4_t *>(page + 16 * (i * kWave + lane));
+            u32x4_t v = *at;
+            const bool odd = clear_odd(v);
+            if (odd)
+                *at = v;
+            any |= odd && (i * kWave + lane) / kPieces < rows;
+        }
+        return any;
     }
 
     static __device__ __forceinline__ float put_back(float o, uint32_t x) {   // x: a bf16 value in the high half
@@ -269,138 +466,131 @@ struct Chunk {
         }
     }
 
-    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, const char *stage, int j, bool masked, int lane) {
-        const int n = lane & 31, h = lane >> 5;
-        f32x16_t s[2];
+    // The ids of a wavefront's pages in consecutive tiles, read four at a time as
+    // scalars (a vector load would have to wait for every page under way).
+    struct Pages {
+        const int32_t *pt;
+        int first, last;   // page of the first tile; the last page of the context
+        int ids[4];
+        __device__ __forceinline__ int next(int i) {   // tiles i = 0, 1, ... of the piece, in order
+            if (i % 4 == 0)
 #pragma unroll
-        for (int kt = 0; kt < 2; kt++) {
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                s[kt][e] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < kKSteps; ks++) {
-                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(stage + k_addr(32 * kt + n, 2 * ks + h));
-                s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf),
-                                                                __builtin_bit_cast(bf16x8_t, st.qf[ks]), s[kt], 0, 0, 0);
-            }
+                for (int k = 0; k < 4; k++)
+                    ids[k] = ld_meta(pt, min(first + (i + k) * kTilePages, last));
+            const int lo = i & 1 ? ids[1] : ids[0], hi = i & 1 ? ids[3] : ids[2];
+            return first_lane_int(i & 2 ? hi : lo);
         }
-        const int room = st.lim - j * kKeyTile - 4 * h;   // key offset 8 (e / 4) + e % 4 + 32 kt is seen if below
-        if (masked) {
-#pragma unroll
-            for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-                for (int e = 0; e < 16; e++)
-                    s[kt][e] = 32 * kt + 8 * (e / 4) + e % 4 < room ? s[kt][e] : -INFINITY;
-        }
-        float mx = s[0][0];
-#pragma unroll
-        for (int kt = 0; kt < 2; kt++)
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                mx = fmaxf(mx, s[kt][e]);
-        mx *= p.scale_log2;
-        if (__any(mx > st.m_ref + kRescaleSlack)) {
-            mx = max_both_halves(mx);
-            const bool up = mx > st.m_ref + kRescaleSlack;
-            // (never zero, so that an infinite sum stays infinite)
-            const float alpha = up ? fmaxf(fast_exp2(st.m_ref - mx), kTiny) : 1.0f;
-            st.m_ref = up ? mx : st.m_ref;
-            st.l *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-#pragma unroll
-                for (int e = 0; e < 16; e++)
-                    st.o[dt][e] *= alpha;
-        }
-        u32x4_t pf[4];   // four steps of 16 keys
-#pragma unroll
-        for (int kt = 0; kt < 2; kt++) {
-#pragma unroll
-            for (int e = 0; e < 16; e++) {
-                float x = fast_exp2(__builtin_fmaf(s[kt][e], p.scale_log2, -st.m_ref));
-                if (masked)
-                    x = 32 * kt + 8 * (e / 4) + e % 4 < room ? x : 0.0f;
-                st.l += x;
-                s[kt][e] = x;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                pf[2 * kt + e / 4][e % 4] = pack_bf16x2(s[kt][2 * e], s[kt][2 * e + 1]);
-        }
-        const char *v = stage + kKBytes;
-#pragma unroll
-        for (int step = 0; step < 4; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(v, dt, step, lane),
-                                                                   __builtin_bit_cast(bf16x8_t, pf[step]), st.o[dt], 0, 0, 0);
+    };
+
+    // Starts loading the first tiles of a piece.
+    __device__ __forceinline__ static Pages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
+        const SeqInfo sq = seq_info(p, pc.b);
+        Pages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
+                    first_lane_int((max(sq.L, 1) - 1) / kPage), {}};
+        const int n = min(pc.j1 - pc.j0, kStages - 1);
+        for (int i = 0; i < n; i++)
+            dma_page(p, st, pages.next(i), pc.g, lds + i * kStage, wave, lane);
+        return pages;
     }
 
-    __device__ __forceinline__ static void piece(const ChunkParams &p, const Piece &pc, int slot, char *lds) {
+    // A worker's range.  While a piece's result is written, the first tiles of
+    // the next one are already on their way.
+    __device__ __forceinline__ static void work(const ChunkParams &p, const uint64_t *s_end, int w, int64_t begin, int64_t end, char *lds) {
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = first_lane_int(threadIdx.x / kWave);
         const int h = lane >> 5;
-        const SeqInfo sq = seq_info(p, pc.b);
-        const int32_t *pt = p.page_table + (size_t)pc.b * p.max_pages;
         const int r = wave * kRowBlock + (lane & 31);
-        const int token = pc.m * p.TT + r / p.G;
-        const bool row_ok = r < p.TT * p.G && token < sq.c.Q;
-        const int head = pc.g * p.G + r % p.G;
-        State st;
-        st.lim = row_ok ? sq.L - sq.c.Q + token + 1 : 0;
-        st.m_ref = -INFINITY;
-        st.l = 0.0f;
-        const uint16_t *qr = p.q + (int64_t)(sq.row0 + (row_ok ? token : 0)) * p.q_stride + (int64_t)(row_ok ? head : 0) * D + 8 * h;
-#pragma unroll
-        for (int ks = 0; ks < kKSteps; ks++) {
-            st.qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + 16 * ks) : u32x4_t{0u, 0u, 0u, 0u};
-            st.qf[ks] ^= p.q_sign;
-        }
-#pragma unroll
-        for (int dt = 0; dt < kDTiles; dt++)
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                st.o[dt][e] = 0.0f;
-        // rows go by token and the valid ones come first, so the wave's first
-        // row sees the fewest keys; what rows without a token hold is not used
-        const int lo_lim = __builtin_amdgcn_readlane(st.lim, 0);
-        int hi_lim = st.lim;
-        for (int d = 16; d; d >>= 1)
-            hi_lim = max(hi_lim, __shfl_xor(hi_lim, d, kWave));
-        hi_lim = first_lane_int(hi_lim);
-
-        Stage sg;
-        load_tile(p, pt, pc.g, pc.j0, sq.L, wave, lane, sg);
-        // the first row of the unit sees the fewest keys
-        const int all_lim = sq.L - sq.c.Q + pc.m * p.TT + 1;
-        bool odd = store_tile(lds, wave, lane, sg, (pc.j0 + 1) * kKeyTile > all_lim);
-        lds_barrier();
-        for (int j = pc.j0; j < pc.j1; j++) {
-            const int cur = (j - pc.j0) & 1;
-            if (j + 1 < pc.j1)
-                load_tile(p, pt, pc.g, j + 1, sq.L, wave, lane, sg);
-            if (j * kKeyTile < hi_lim)
-                tile_step(p, st, lds + cur * kStage, j, (j + 1) * kKeyTile > lo_lim, lane);
-            if (j + 1 < pc.j1)
-                odd |= store_tile(lds + (cur ^ 1) * kStage, wave, lane, sg, (j + 2) * kKeyTile > all_lim);
-            lds_barrier();
-        }
-        if (pc.j1 * kKeyTile > all_lim) {   // the same for every wavefront
-            int *flags = reinterpret_cast<int *>(lds);
-            const bool mine = __any(odd);
-            if (lane == 0)
-                flags[wave] = mine;
-            lds_barrier();
-            bool any = false;
-#pragma unroll
-            for (int i = 0; i < kChunkWaves; i++)
-                any |= flags[i] != 0;
-            lds_barrier();
-            if (any)
-                add_odd(p, st, pt, pc.g, max(pc.j0, max(all_lim, 0) / kKeyTile) * kKeyTile, min(pc.j1 * kKeyTile, sq.L), h);
-        }
-        if (!row_ok)
+        int64_t x = begin;
+        Piece pc;
+        if (!next_piece(p, s_end, x, end, false, pc))
             return;
+        bool first = pc.us + pc.j0 == begin;   // the range starts with it: its partial result's slot
+        State st;
+        set_addresses(st, lds, wave, lane);
+        Pages pages = start(p, st, pc, lds, wave, lane);
+        for (;;) {
+            const SeqInfo sq = seq_info(p, pc.b);
+            const int token = pc.m * p.TT + r / p.G;
+            const bool row_ok = r < p.TT * p.G && token < sq.c.Q;
+            const int head = pc.g * p.G + r % p.G;
+            // the first row of the unit sees the fewest keys; tiles before
+            // `plain` are seen whole by every row, and lie inside the context
+            const int all_lim = sq.L - sq.c.Q + pc.m * p.TT + 1;
+            const int plain = first_lane_int(min(max(max(all_lim, 0) / kKeyTile, pc.j0), pc.j1));
+            st.lim = row_ok ? sq.L - sq.c.Q + token + 1 : 0;
+            st.m_ref = -INFINITY;
+            st.l = 0.0f;
+            const uint16_t *qr = p.q + (int64_t)(sq.row0 + (row_ok ? token : 0)) * p.q_stride + (int64_t)(row_ok ? head : 0) * D + 8 * h;
+#pragma unroll
+            for (int ks = 0; ks < kKSteps; ks++) {
+                st.qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + 16 * ks) : u32x4_t{0u, 0u, 0u, 0u};
+                st.qf[ks] ^= p.q_sign;
+            }
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    st.o[dt][e] = 0.0f;
+            int hi_lim = st.lim;   // keys that the wavefront's last row sees
+            for (int d = 16; d; d >>= 1)
+                hi_lim = max(hi_lim, __shfl_xor(hi_lim, d, kWave));
+            hi_lim = first_lane_int(hi_lim);
+
+            // After the barrier a tile is there, and nobody reads the one before
+            // it any more, whose stage is filled next.
+            const int n = pc.j1 - pc.j0, n_plain = plain - pc.j0;
+            const auto meet = [&](int i) __attribute__((always_inline)) {
+                lds_barrier();
+                if (i + kStages - 1 < n)
+                    dma_page(p, st, pages.next(i + kStages - 1), pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
+            };
+            const bool any_row = hi_lim > 0;
+            for (int i = 0; i < n_plain; i++) {
+                dma_wait<kLoads>(n - 1 - i);
+                meet(i);
+                if (any_row)
+                    tile_step<false>(p, st, i % kStages * kStage, 0);
+            }
+            // the tiles that some row does not see whole
+            bool odd = false;
+            for (int i = n_plain; i < n; i++) {
+                const int stage = i % kStages * kStage, j = pc.j0 + i;
+                dma_wait<kLoads>(n - 1 - i);
+                if (wave >= kTilePages)
+                    odd |= clean_page(lds + stage, wave, lane, sq.L - (j * kTilePages + wave % kTilePages) * kPage);
+                meet(i);
+                if (j * kKeyTile < hi_lim)
+                    tile_step<true>(p, st, stage, st.lim - j * kKeyTile - 4 * h);
+            }
+            lds_barrier();
+            if (n_plain < n) {   // the same for every wavefront
+                int *flags = reinterpret_cast<int *>(lds + (kStages - 1) * kStage);   // the stage that start() leaves alone
+                const bool mine = __any(odd);
+                if (lane == 0)
+                    flags[wave] = mine;
+                lds_barrier();
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < kChunkWaves; i++)
+                    any |= flags[i] != 0;
+                if (any)
+                    add_odd(p, st, p.page_table + (size_t)pc.b * p.max_pages, pc.g, plain * kKeyTile, min(pc.j1 * kKeyTile, sq.L), h);
+            }
+            Piece nx = pc;
+            const bool more = next_piece(p, s_end, x, end, true, nx);
+            if (more)
+                pages = start(p, st, nx, lds, wave, lane);
+            if (row_ok)
+                write_rows(p, st, sq, pc, first ? 2 * w : 2 * w + 1, r, token, head, h);
+            if (!more)
+                return;
+            pc = nx;
+            first = false;
+        }
+    }
+
+    __device__ __forceinline__ static void write_rows(const ChunkParams &p, const State &st, const SeqInfo &sq, const Piece &pc, int slot, int r,
+                                      int token, int head, int h) {
         const float l = sum_both_halves(st.l);
         const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // NaN stays
         if (pc.whole) {
@@ -433,18 +623,14 @@ struct Chunk {
 
 template <int D>
 __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(ChunkParams p) {
-    extern __shared__ uint64_t s_tiles[];
-    char *lds = reinterpret_cast<char *>(s_tiles) + (((p.B + 1) * 8 + 127) & ~127);
-    tile_prefix(p, s_tiles);
-    const int64_t ptot = (int64_t)s_tiles[p.B] * p.Hkv;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];   // the tiles, then the prefix
+    uint64_t *s_tiles = reinterpret_cast<uint64_t *>(lds + Chunk<D>::kLds);
+    tile_ends(p, s_tiles);
+    const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
     const int w = xcd_worker(blockIdx.x, p.W);
     const int64_t begin = first_lane_int64(range_start(ptot, w, p.W, p.range_inv));
     const int64_t end = first_lane_int64(range_start(ptot, w + 1, p.W, p.range_inv));
-    for (int64_t x = begin; x < end;) {
-        const Piece pc = locate_tile(p, s_tiles, x, end);
-        Chunk<D>::piece(p, pc, x == begin ? 2 * w : 2 * w + 1, lds);
-        x = pc.next;
-    }
+    Chunk<D>::work(p, s_tiles, w, begin, end, lds);
 }
 
 // Joins the pieces of the units that a worker boundary cuts: workgroup x takes
@@ -455,16 +641,16 @@ constexpr int kMergeRows = 32;
 template <int D>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
     extern __shared__ uint64_t s_tiles[];
-    tile_prefix(p, s_tiles);
-    const int64_t ptot = (int64_t)s_tiles[p.B] * p.Hkv;
+    tile_ends(p, s_tiles);
+    const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
     const int w = blockIdx.x + 1;
     const int64_t x = first_lane_int64(range_start(ptot, w, p.W, p.range_inv));
     const int64_t prev = first_lane_int64(range_start(ptot, w - 1, p.W, p.range_inv));
     if (x >= ptot || x == prev)
         return;
     const Piece pc = locate_tile(p, s_tiles, x, ptot);
-    if (x == pc.us || prev > pc.us)
-        return;   // not cut here, or an earlier boundary cuts it too
+    if (x == pc.us || x >= pc.us + pc.n || prev > pc.us)
+        return;   // no tiles are cut off here, or an earlier boundary cuts the unit too
     const UnitSplit u = unit_split(ptot, pc.us, pc.n, p.W);
     const SeqInfo sq = seq_info(p, pc.b);
     constexpr int kPer = D / 8;   // values of a thread, eight threads per row
@@ -516,7 +702,7 @@ int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
     // KV tiles of the call, from above
     const int64_t tiles = ((int64_t)s->num_tokens / pl->TT + std::min(s->num_seqs, s->num_tokens)) * s->num_kv_heads *
                           (((int64_t)s->max_ctx_len + kKeyTile - 1) / kKeyTile);
-    pl->W = s->num_workers > 0 ? s->num_workers : (int)std::max<int64_t>(1, std::min<int64_t>(512, tiles / 2));
+    pl->W = s->num_workers > 0 ? s->num_workers : (int)std::max<int64_t>(1, std::min<int64_t>(256, tiles / 2));
     const size_t rows = 2 * (size_t)pl->W * kTileRows;
     pl->ws_lse_off = rows * s->head_dim * sizeof(float);
     pl->ws_bytes = (pl->ws_lse_off + rows * sizeof(float) + 255) & ~(size_t)255;
@@ -622,7 +808,7 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     p.range_inv = range_reciprocal(pl.W);
     p.scale_log2 = std::fabs(scale) * 1.44269504088896341f;
     p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
-    const size_t pre = (((size_t)s->num_seqs + 1) * 8 + 127) & ~(size_t)127;
+    const size_t pre = (size_t)s->num_seqs * sizeof(uint64_t);
     const bool small = s->head_dim == 64;
     const auto main_k = small ? chunk_attn_kernel<64> : chunk_attn_kernel<128>;
     const auto merge_k = small ? chunk_merge_kernel<64> : chunk_merge_kernel<128>;

@@ -5,7 +5,10 @@
 // A sequence of context length L with Q new tokens is cut into row tiles of TT
 // tokens.  Row tile j (from 0) ends at token min(Q, (j + 1) TT) and sees the
 // keys up to that token, so it takes ceil((P + min(Q, (j + 1) TT)) / 64) KV
-// tiles of 64 keys, P = max(L - Q, 0) (tokens in front of the chunk).
+// tiles of 64 keys, P = max(L - Q, 0) (tokens in front of the chunk).  Its
+// share of the line of work is kUnitTiles longer: behind its KV tiles lie that
+// many places without any, so that workers with many short row tiles get
+// fewer KV tiles.
 #pragma once
 
 #include <stdint.h>
@@ -15,6 +18,7 @@
 namespace tsattn {
 
 constexpr int kKeyTile = 64;   // keys per KV tile
+constexpr int kUnitTiles = 6;  // what starting and ending a row tile costs, in KV tiles
 
 // sum over i = 0 .. n - 1 of floor((a i + b) / 64), for n <= 2^23, a <= 256:
 // whole multiples of 64 leave a and b, then the roles of the axes are swapped
@@ -52,13 +56,13 @@ struct ChunkSeq {
         return P + (int)(e < Q ? e : Q);
     }
     TS_HOST_DEVICE int cost(int j) const { return (keys_end(j) + kKeyTile - 1) / kKeyTile; }
-    // KV tiles of row tiles 0 .. j - 1
+    // places of row tiles 0 .. j - 1
     TS_HOST_DEVICE int64_t before(int j) const {
         const int full = Q / TT, n = j < full ? j : full;
         int64_t c = floor_sum64((uint32_t)n, (uint32_t)TT, (uint64_t)P + TT + kKeyTile - 1);
         if (j > full)
             c += cost(full);
-        return c;
+        return c + (int64_t)j * kUnitTiles;
     }
     TS_HOST_DEVICE int64_t total() const { return before(tiles()); }
 };

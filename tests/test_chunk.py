@@ -112,7 +112,7 @@ int main() {
             int tiles = 0;
             for (long t = 0; t < (long)s.P + last; t += 64) tiles++;
             if (s.P < 5000 && tiles != s.cost(j)) { printf("cost(%d): Q %d P %d TT %d\n", j, s.Q, s.P, s.TT); return 1; }
-            c += s.cost(j);
+            c += s.cost(j) + kUnitTiles;
             row = last;
             n++;
         }
@@ -120,7 +120,7 @@ int main() {
     }
     ChunkSeq s{1 << 22, 1 << 30, 8};   // the largest chunk behind the longest context
     int64_t c = 0;
-    for (int j = 0; j < s.tiles(); j++) c += s.cost(j);
+    for (int j = 0; j < s.tiles(); j++) c += s.cost(j) + kUnitTiles;
     if (c != s.total()) return 1;
     printf("ok %ld\n", n);
     return 0;
