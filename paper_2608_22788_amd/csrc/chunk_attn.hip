@@ -23,6 +23,7 @@ constexpr int kChunkWaves = 8;
 constexpr int kStages = 4;         // KV tiles in LDS: one in use, the others on their way
 constexpr int kTileRows = kChunkWaves * kRowBlock;
 constexpr float kTiny = 1.17549435e-38f;   // the smallest normal float32
+constexpr float kLowest = -3.0e38f;       // the reference of a row without a score yet
 constexpr int kTilePages = kKeyTile / kPage;
 
 struct ChunkParams {
@@ -298,17 +299,13 @@ struct Chunk {
         return __builtin_bit_cast(bf16x8_t, ab);
     }
 
-    __device__ __forceinline__ static float max16(const f32x16_t &s) {
-        float m = fmaxf(s[0], s[1]);
-#pragma unroll
-        for (int e = 2; e < 16; e += 2)
-            m = fmaxf(fmaxf(m, s[e]), s[e + 1]);
-        return m;
-    }
+    struct Scores {
+        f32x16_t s[2];   // keys 32 kt + 8 (e / 4) + 4 h + e % 4 of this lane's row in s[kt][e]
+        float mx;        // the largest, times the scale
+    };
 
-    // Raises the reference where a score exceeds it by more than the slack;
-    // `pf`, if any, holds weights that were taken with the old one.
-    __device__ __forceinline__ static void raise(State &st, float mx, u32x4_t *pf) {
+    // Raises the reference where a score exceeds it by more than the slack.
+    __device__ __forceinline__ static void raise(State &st, float mx) {
         if (__builtin_expect(__any(mx > st.m_ref + kRescaleSlack), 0)) {
             mx = max_both_halves(mx);
             const bool up = mx > st.m_ref + kRescaleSlack;
@@ -321,88 +318,90 @@ struct Chunk {
 #pragma unroll
                 for (int e = 0; e < 16; e++)
                     st.o[dt][e] *= alpha;
-            if (pf)
-#pragma unroll
-                for (int i = 0; i < 8; i++)
-                    pf[i / 4][i % 4] = pack_bf16x2(bf16_lo(pf[i / 4][i % 4]) * alpha, bf16_hi(pf[i / 4][i % 4]) * alpha);
         }
     }
 
     // Weights of 32 keys, packed in the order of the value operand.
-    template <bool kMasked>
-    __device__ __forceinline__ static void weights(const ChunkParams &p, State &st, f32x16_t &s, int room, u32x4_t (&pf)[2]) {
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-            float x = fast_exp2(__builtin_fmaf(s[e], p.scale_log2, -st.m_ref));
-            if constexpr (kMasked)
-                x = 8 * (e / 4) + e % 4 < room ? x : 0.0f;
-            s[e] = x;
-        }
-        float sum = 0.0f;
+    __device__ __forceinline__ static void weights(const ChunkParams &p, State &st, const f32x16_t &s, u32x4_t (&pf)[2]) {
+        float x[16];
 #pragma unroll
         for (int e = 0; e < 16; e++)
-            sum += s[e];
-        st.l += sum;
+            x[e] = fast_exp2(__builtin_fmaf(s[e], p.scale_log2, -st.m_ref));
 #pragma unroll
         for (int e = 0; e < 8; e++)
-            pf[e / 4][e % 4] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
+            pf[e / 4][e % 4] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+        float even = x[0], odd = x[1];
+#pragma unroll
+        for (int e = 2; e < 16; e += 2) {
+            even += x[e];
+            odd += x[e + 1];
+        }
+        st.l += even + odd;
     }
 
-    template <bool kMasked>
-    __device__ __forceinline__ static void mask(f32x16_t &s, int room) {
-        if constexpr (kMasked)
+    __device__ __forceinline__ static void scores(const State &st, int stage, Scores &n) {
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++) {
+            f32x16_t s = {};
+#pragma unroll
+            for (int ks = 0; ks < kKSteps; ks++)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(st, stage, kt, ks), __builtin_bit_cast(bf16x8_t, st.qf[ks]), s, 0, 0, 0);
+            n.s[kt] = s;
+        }
+    }
+    // Scores of keys that the row does not see: their weight is exactly zero,
+    // since the reference is finite.
+    __device__ __forceinline__ static void mask(Scores &n, int room) {
+#pragma unroll
+        for (int kt = 0; kt < 2; kt++)
 #pragma unroll
             for (int e = 0; e < 16; e++)
-                s[e] = 8 * (e / 4) + e % 4 < room ? s[e] : -INFINITY;
+                n.s[kt][e] = 32 * kt + 8 * (e / 4) + e % 4 < room ? n.s[kt][e] : -INFINITY;
+    }
+    __device__ __forceinline__ static void largest(const ChunkParams &p, Scores &n) {
+        float m = fmaxf(n.s[0][0], n.s[0][1]);
+#pragma unroll
+        for (int e = 2; e < 32; e += 2)
+            m = fmaxf(fmaxf(m, n.s[e / 16][e % 16]), n.s[e / 16][e % 16 + 1]);
+        n.mx = m * p.scale_log2;
     }
 
-    // One KV tile.  The two halves of 32 keys overlap: the second half's score
-    // products run while the first half's weights are taken, the first half's
-    // value products while the second's are.
-    // `stage` is its byte offset; masked, the key of a lane's register e of half
-    // kt is seen if 32 kt + 8 (e / 4) + e % 4 is below `room`.
-    template <bool kMasked>
-    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, int stage, int room) {
-        const f32x16_t zero = {};
-        f32x16_t s0 = zero, s1 = zero;
-        bf16x8_t a[kKSteps], c[kKSteps];
-#pragma unroll
-        for (int ks = 0; ks < kKSteps; ks++)
-            a[ks] = k_frag(st, stage, 0, ks);
-#pragma unroll
-        for (int ks = 0; ks < kKSteps; ks++) {
-            s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], __builtin_bit_cast(bf16x8_t, st.qf[ks]), s0, 0, 0, 0);
-            c[ks] = k_frag(st, stage, 1, ks);
-        }
-        mask<kMasked>(s0, room);
-        raise(st, max16(s0) * p.scale_log2, nullptr);
-        u32x4_t p0[2], p1[2];
+    // One KV tile, whose scores are `c`, and (kNext) the scores `n` of the next
+    // one.  The matrix products of the next scores run beside the weights of the
+    // first 32 keys, the value products beside those of the other 32 and the
+    // next maximum.  `room` (masked): keys of the next tile that the lane's row
+    // sees, less 4 h.
+    template <bool kNext>
+    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, const Scores &c, Scores &n, int v_stage, int k_stage,
+                                     bool masked, int room) {
+        raise(st, c.mx);
+        u32x4_t pf[2][2];
         bf16x8_t v0[2][kDTiles];
-#pragma unroll
-        for (int ks = 0; ks < kKSteps; ks++)
-            s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[ks], __builtin_bit_cast(bf16x8_t, st.qf[ks]), s1, 0, 0, 0);
-        weights<kMasked>(p, st, s0, room, p0);
-#pragma unroll
-        for (int step = 0; step < 2; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-                v0[step][dt] = v_frag(st, stage, dt, step);
-        mask<kMasked>(s1, room - 32);
-        raise(st, max16(s1) * p.scale_log2, p0);
-        bf16x8_t v1[2][kDTiles];
-#pragma unroll
-        for (int step = 0; step < 2; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++) {
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[step][dt], __builtin_bit_cast(bf16x8_t, p0[step]), st.o[dt], 0, 0, 0);
-                v1[step][dt] = v_frag(st, stage, dt, 2 + step);
-            }
-        weights<kMasked>(p, st, s1, room - 32, p1);
+        if constexpr (kNext)
+            scores(st, k_stage, n);
+        weights(p, st, c.s[0], pf[0]);
 #pragma unroll
         for (int step = 0; step < 2; step++)
 #pragma unroll
             for (int dt = 0; dt < kDTiles; dt++)
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1[step][dt], __builtin_bit_cast(bf16x8_t, p1[step]), st.o[dt], 0, 0, 0);
+                v0[step][dt] = v_frag(st, v_stage, dt, step);
+        if constexpr (kNext)
+            if (__builtin_expect(masked, 0))
+                mask(n, room);
+#pragma unroll
+        for (int step = 0; step < 2; step++)
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[step][dt], __builtin_bit_cast(bf16x8_t, pf[0][step]), st.o[dt], 0, 0, 0);
+        weights(p, st, c.s[1], pf[1]);
+#pragma unroll
+        for (int step = 0; step < 2; step++)
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; dt++)
+                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(st, v_stage, dt, 2 + step), __builtin_bit_cast(bf16x8_t, pf[1][step]),
+                                                                   st.o[dt], 0, 0, 0);
+        if constexpr (kNext)
+            largest(p, n);
     }
 
     // Infinite and NaN values.  Where a row does not see a key, the key's zero
@@ -518,7 +517,7 @@ struct Chunk {
             const int all_lim = sq.L - sq.c.Q + pc.m * p.TT + 1;
             const int plain = first_lane_int(min(max(max(all_lim, 0) / kKeyTile, pc.j0), pc.j1));
             st.lim = row_ok ? sq.L - sq.c.Q + token + 1 : 0;
-            st.m_ref = -INFINITY;
+            st.m_ref = kLowest;
             st.l = 0.0f;
             const uint16_t *qr = p.q + (int64_t)(sq.row0 + (row_ok ? token : 0)) * p.q_stride + (int64_t)(row_ok ? head : 0) * D + 8 * h;
 #pragma unroll
@@ -531,36 +530,46 @@ struct Chunk {
 #pragma unroll
                 for (int e = 0; e < 16; e++)
                     st.o[dt][e] = 0.0f;
-            int hi_lim = st.lim;   // keys that the wavefront's last row sees
-            for (int d = 16; d; d >>= 1)
-                hi_lim = max(hi_lim, __shfl_xor(hi_lim, d, kWave));
-            hi_lim = first_lane_int(hi_lim);
-
-            // After the barrier a tile is there, and nobody reads the one before
-            // it any more, whose stage is filled next.
+            // Tile i is used by two steps: its keys by step i - 1, its values by
+            // step i.  After the barrier in front of step i tile i + 1 is there,
+            // and nobody reads tile i - 1 any more, whose stage is filled next.
             const int n = pc.j1 - pc.j0, n_plain = plain - pc.j0;
-            const auto meet = [&](int i) __attribute__((always_inline)) {
+            bool odd = false;
+            const auto arrive = [&](int i, int later) __attribute__((always_inline)) {
+                dma_wait<kLoads>(later);
+                if (i >= n_plain && wave >= kTilePages)
+                    odd |= clean_page(lds + i % kStages * kStage, wave, lane, sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage);
                 lds_barrier();
+            };
+            const auto room = [&](int i) { return st.lim - (pc.j0 + i) * kKeyTile - 4 * h; };
+            const auto advance = [&](int i) __attribute__((always_inline)) {
+                arrive(i + 1, min(n - 2 - i, 1));
                 if (i + kStages - 1 < n)
                     dma_page(p, st, pages.next(i + kStages - 1), pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
-            const bool any_row = hi_lim > 0;
-            for (int i = 0; i < n_plain; i++) {
-                dma_wait<kLoads>(n - 1 - i);
-                meet(i);
-                if (any_row)
-                    tile_step<false>(p, st, i % kStages * kStage, 0);
-            }
-            // the tiles that some row does not see whole
-            bool odd = false;
-            for (int i = n_plain; i < n; i++) {
-                const int stage = i % kStages * kStage, j = pc.j0 + i;
-                dma_wait<kLoads>(n - 1 - i);
-                if (wave >= kTilePages)
-                    odd |= clean_page(lds + stage, wave, lane, sq.L - (j * kTilePages + wave % kTilePages) * kPage);
-                meet(i);
-                if (j * kKeyTile < hi_lim)
-                    tile_step<true>(p, st, stage, st.lim - j * kKeyTile - 4 * h);
+            const auto step = [&](int i, const Scores &c, Scores &next) __attribute__((always_inline)) {
+                advance(i);
+                tile_step<true>(p, st, c, next, i % kStages * kStage, (i + 1) % kStages * kStage, i + 1 >= n_plain, room(i + 1));
+            };
+            arrive(0, min(n - 1, 2));
+            if (__any(row_ok)) {
+                Scores a, b;
+                scores(st, 0, a);
+                if (n_plain == 0)
+                    mask(a, room(0));
+                largest(p, a);
+                for (int i = 0; i + 1 < n; i += 2) {
+                    step(i, a, b);
+                    if (i + 2 >= n) {
+                        a = b;
+                        break;
+                    }
+                    step(i + 1, b, a);
+                }
+                tile_step<false>(p, st, a, b, (n - 1) % kStages * kStage, 0, false, 0);
+            } else {   // no row of this wavefront has a token: it only loads
+                for (int i = 0; i + 1 < n; i++)
+                    advance(i);
             }
             lds_barrier();
             if (n_plain < n) {   // the same for every wavefront
@@ -806,7 +815,9 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     p.TT = pl.TT;
     p.W = pl.W;
     p.range_inv = range_reciprocal(pl.W);
-    p.scale_log2 = std::fabs(scale) * 1.44269504088896341f;
+    // (a scale of 0 leaves equal scores, but no product of it with the -inf of a
+    // masked one)
+    p.scale_log2 = std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f);
     p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
     const size_t pre = (size_t)s->num_seqs * sizeof(uint64_t);
     const bool small = s->head_dim == 64;
