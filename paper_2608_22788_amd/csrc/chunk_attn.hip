@@ -321,24 +321,6 @@ struct Chunk {
         }
     }
 
-    // Weights of 32 keys, packed in the order of the value operand.
-    __device__ __forceinline__ static void weights(const ChunkParams &p, State &st, const f32x16_t &s, u32x4_t (&pf)[2]) {
-        float x[16];
-#pragma unroll
-        for (int e = 0; e < 16; e++)
-            x[e] = fast_exp2(__builtin_fmaf(s[e], p.scale_log2, -st.m_ref));
-#pragma unroll
-        for (int e = 0; e < 8; e++)
-            pf[e / 4][e % 4] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-        float even = x[0], odd = x[1];
-#pragma unroll
-        for (int e = 2; e < 16; e += 2) {
-            even += x[e];
-            odd += x[e + 1];
-        }
-        st.l += even + odd;
-    }
-
     __device__ __forceinline__ static void scores(const State &st, int stage, Scores &n) {
 #pragma unroll
         for (int kt = 0; kt < 2; kt++) {
@@ -367,41 +349,79 @@ struct Chunk {
     }
 
     // One KV tile, whose scores are `c`, and (kNext) the scores `n` of the next
-    // one.  The matrix products of the next scores run beside the weights of the
-    // first 32 keys, the value products beside those of the other 32 and the
-    // next maximum.  `room` (masked): keys of the next tile that the lane's row
-    // sees, less 4 h.
+    // one.  `room` (masked): keys of the tile that the lane's row sees, less 4 h.
     template <bool kNext>
-    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, const Scores &c, Scores &n, int v_stage, int k_stage,
+    __device__ __forceinline__ static void tile_step(const ChunkParams &p, State &st, Scores &c, Scores &n, int v_stage, int k_stage,
                                      bool masked, int room) {
+        if (__builtin_expect(masked, 0)) {
+            mask(c, room);
+            largest(p, c);
+        }
         raise(st, c.mx);
+        // From here on nothing branches, and the order of the instructions is
+        // the one written here (sched_fence): each matrix product is followed by
+        // the vector instructions that fit beside it and the operand of the
+        // product four later.  The next scores' products stand beside the
+        // weights of the first 32 keys, the value products beside those of the
+        // other 32, then the next maximum.
+        constexpr int kAhead = 4, kScore = 2 * kKSteps, kValue = 4 * kDTiles;
         u32x4_t pf[2][2];
-        bf16x8_t v0[2][kDTiles];
+        bf16x8_t kf[kAhead], vf[kAhead];
+        float x[2][16], sum[2] = {0.0f, 0.0f}, m[2] = {-INFINITY, -INFINITY};
+        const auto weigh = [&](int half, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = from; e < to; e++) {
+                x[half][e] = fast_exp2(__builtin_fmaf(c.s[half][e], p.scale_log2, -st.m_ref));
+                if (e % 2) {
+                    pf[half][e / 8][e / 2 % 4] = pack_bf16x2(x[half][e - 1], x[half][e]);
+                    sum[0] += x[half][e - 1];
+                    sum[1] += x[half][e];
+                }
+            }
+        };
+        const auto values = [&](int i) { return v_frag(st, v_stage, i % kDTiles, i / kDTiles); };
+        if constexpr (kNext) {
+            const f32x16_t zero = {};
+            n.s[0] = n.s[1] = zero;
+#pragma unroll
+            for (int i = 0; i < kAhead; i++)
+                kf[i] = k_frag(st, k_stage, i / kKSteps, i % kKSteps);
+            sched_fence();
+#pragma unroll
+            for (int i = 0; i < kScore; i++) {
+                n.s[i / kKSteps] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kAhead], __builtin_bit_cast(bf16x8_t, st.qf[i % kKSteps]),
+                                                                           n.s[i / kKSteps], 0, 0, 0);
+                if (i + kAhead < kScore)
+                    kf[i % kAhead] = k_frag(st, k_stage, (i + kAhead) / kKSteps, (i + kAhead) % kKSteps);
+                else
+                    vf[i + kAhead - kScore] = values(i + kAhead - kScore);
+                weigh(0, i * 16 / kScore, (i + 1) * 16 / kScore);
+                sched_fence();
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; i++)
+                vf[i] = values(i);
+            weigh(0, 0, 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kValue; i++) {
+            f32x16_t &o = st.o[i % kDTiles];
+            const int step = i / kDTiles;
+            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], __builtin_bit_cast(bf16x8_t, pf[step / 2][step % 2]), o, 0, 0, 0);
+            if (i + kAhead < kValue)
+                vf[i % kAhead] = values(i + kAhead);
+            if (i < kValue / 2)
+                weigh(1, i * 32 / kValue, (i + 1) * 32 / kValue);
+            else if constexpr (kNext)
+#pragma unroll
+                for (int e = (i - kValue / 2) * 64 / kValue; e < (i - kValue / 2 + 1) * 64 / kValue; e += 2)
+                    m[e / 2 % 2] = fmaxf(fmaxf(m[e / 2 % 2], n.s[e / 16][e % 16]), n.s[e / 16][e % 16 + 1]);
+            sched_fence();
+        }
+        st.l += sum[0] + sum[1];
         if constexpr (kNext)
-            scores(st, k_stage, n);
-        weights(p, st, c.s[0], pf[0]);
-#pragma unroll
-        for (int step = 0; step < 2; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-                v0[step][dt] = v_frag(st, v_stage, dt, step);
-        if constexpr (kNext)
-            if (__builtin_expect(masked, 0))
-                mask(n, room);
-#pragma unroll
-        for (int step = 0; step < 2; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0[step][dt], __builtin_bit_cast(bf16x8_t, pf[0][step]), st.o[dt], 0, 0, 0);
-        weights(p, st, c.s[1], pf[1]);
-#pragma unroll
-        for (int step = 0; step < 2; step++)
-#pragma unroll
-            for (int dt = 0; dt < kDTiles; dt++)
-                st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(st, v_stage, dt, 2 + step), __builtin_bit_cast(bf16x8_t, pf[1][step]),
-                                                                   st.o[dt], 0, 0, 0);
-        if constexpr (kNext)
-            largest(p, n);
+            n.mx = fmaxf(m[0], m[1]) * p.scale_log2;
     }
 
     // Infinite and NaN values.  Where a row does not see a key, the key's zero
@@ -547,16 +567,14 @@ struct Chunk {
                 if (i + kStages - 1 < n)
                     dma_page(p, st, pages.next(i + kStages - 1), pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
-            const auto step = [&](int i, const Scores &c, Scores &next) __attribute__((always_inline)) {
+            const auto step = [&](int i, Scores &c, Scores &next) __attribute__((always_inline)) {
                 advance(i);
-                tile_step<true>(p, st, c, next, i % kStages * kStage, (i + 1) % kStages * kStage, i + 1 >= n_plain, room(i + 1));
+                tile_step<true>(p, st, c, next, i % kStages * kStage, (i + 1) % kStages * kStage, i >= n_plain, room(i));
             };
             arrive(0, min(n - 1, 2));
             if (__any(row_ok)) {
                 Scores a, b;
                 scores(st, 0, a);
-                if (n_plain == 0)
-                    mask(a, room(0));
                 largest(p, a);
                 for (int i = 0; i + 1 < n; i += 2) {
                     step(i, a, b);
@@ -566,7 +584,7 @@ struct Chunk {
                     }
                     step(i + 1, b, a);
                 }
-                tile_step<false>(p, st, a, b, (n - 1) % kStages * kStage, 0, false, 0);
+                tile_step<false>(p, st, a, b, (n - 1) % kStages * kStage, 0, n > n_plain, room(n - 1));
             } else {   // no row of this wavefront has a token: it only loads
                 for (int i = 0; i + 1 < n; i++)
                     advance(i);
