@@ -378,6 +378,7 @@ struct Chunk {
                     sum[1] += x[half][e];
                 }
             }
+            asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));   // (here, not at the end of the step: 1.7 %)
         };
         const auto values = [&](int i) { return v_frag(st, v_stage, i % kDTiles, i / kDTiles); };
         if constexpr (kNext) {
@@ -413,10 +414,12 @@ struct Chunk {
                 vf[i % kAhead] = values(i + kAhead);
             if (i < kValue / 2)
                 weigh(1, i * 32 / kValue, (i + 1) * 32 / kValue);
-            else if constexpr (kNext)
+            else if constexpr (kNext) {
 #pragma unroll
                 for (int e = (i - kValue / 2) * 64 / kValue; e < (i - kValue / 2 + 1) * 64 / kValue; e += 2)
                     m[e / 2 % 2] = fmaxf(fmaxf(m[e / 2 % 2], n.s[e / 16][e % 16]), n.s[e / 16][e % 16 + 1]);
+                asm volatile("" : "+v"(m[0]), "+v"(m[1]));
+            }
             sched_fence();
         }
         st.l += sum[0] + sum[1];
@@ -662,11 +665,15 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(Chun
 
 // Joins the pieces of the units that a worker boundary cuts: workgroup x takes
 // the unit that boundary x + 1 falls into, if it is the first one inside it;
-// workgroups along y take kMergeRows rows each.
-constexpr int kMergeRows = 32;
+// workgroups along y take merge_rows(D) rows each, D / 8 lanes per row.  The
+// loads of several pieces are under way at once: one after the other, sixteen
+// pieces took 21 us.
+constexpr int kMergeThreads = 256, kMergeAhead = 4;
+constexpr int merge_rows(int D) { return kMergeThreads / (D / 8); }
 
 template <int D>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
+__global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams p) {
+    constexpr int kMergeRows = merge_rows(D), kMergeLanes = D / 8;
     extern __shared__ uint64_t s_tiles[];
     tile_ends(p, s_tiles);
     const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
@@ -680,31 +687,42 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
         return;   // no tiles are cut off here, or an earlier boundary cuts the unit too
     const UnitSplit u = unit_split(ptot, pc.us, pc.n, p.W);
     const SeqInfo sq = seq_info(p, pc.b);
-    constexpr int kPer = D / 8;   // values of a thread, eight threads per row
-    const int r = blockIdx.y * kMergeRows + threadIdx.x / 8, part = threadIdx.x % 8;
+    constexpr int kPer = D / kMergeLanes;
+    const int r = blockIdx.y * kMergeRows + threadIdx.x / kMergeLanes, part = threadIdx.x % kMergeLanes;
     const int token = pc.m * p.TT + r / p.G;
     if (r >= p.TT * p.G || token >= sq.c.Q)
-        return;
+        return;   // (whole rows of lanes)
+    const auto row_of = [&](int k) { return (int64_t)u.slot(k) * kTileRows + r; };
     float M = -INFINITY;
-    for (int k = 0; k < u.nparts; k++)
-        M = fmaxf(M, p.ws_lse[(int64_t)u.slot(k) * kTileRows + r]);
+    for (int k = part; k < u.nparts; k += kMergeLanes)
+        M = fmaxf(M, p.ws_lse[row_of(k)]);
+#pragma unroll
+    for (int d = 1; d < kMergeLanes; d *= 2)
+        M = fmaxf(M, __shfl_xor(M, d, kWave));
     float sum = 0.0f, o[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; e++)
         o[e] = 0.0f;
-    for (int k = 0; k < u.nparts; k++) {
-        const int64_t row = (int64_t)u.slot(k) * kTileRows + r;
-        const float lse = p.ws_lse[row];
-        if (lse == -INFINITY)
-            continue;
-        const float a = fmaxf(fast_exp2(lse - M), kTiny);   // an infinite piece stays infinite
-        sum += a;
+    for (int k0 = 0; k0 < u.nparts; k0 += kMergeAhead) {
+        f32x4_t v[kMergeAhead][kPer / 4];
+        float lse[kMergeAhead];
 #pragma unroll
-        for (int e = 0; e < kPer; e += 4) {
-            const f32x4_t x4 = *reinterpret_cast<const f32x4_t *>(p.ws_o + row * D + kPer * part + e);
+        for (int i = 0; i < kMergeAhead; i++) {
+            const int64_t row = row_of(min(k0 + i, u.nparts - 1));
+            lse[i] = p.ws_lse[row];
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                o[e + i] += a * x4[i];
+            for (int e = 0; e < kPer / 4; e++)
+                v[i][e] = *reinterpret_cast<const f32x4_t *>(p.ws_o + row * D + kPer * part + 4 * e);
+        }
+#pragma unroll
+        for (int i = 0; i < kMergeAhead; i++) {
+            if (k0 + i >= u.nparts || lse[i] == -INFINITY)   // past the end, or a piece without a visible key
+                continue;
+            const float a = fmaxf(fast_exp2(lse[i] - M), kTiny);   // an infinite piece stays infinite
+            sum += a;
+#pragma unroll
+            for (int e = 0; e < kPer; e++)
+                o[e] += a * v[i][e / 4][e % 4];
         }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -848,7 +866,8 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     if (e != hipSuccess)
         return hip_fail(e, "chunk attention launch");
     if (pl.W > 1) {
-        hipLaunchKernelGGL(merge_k, dim3((unsigned)pl.W - 1, kTileRows / kMergeRows), dim3(256), pre, hs, p);
+        hipLaunchKernelGGL(merge_k, dim3((unsigned)pl.W - 1, kTileRows / merge_rows(s->head_dim)), dim3(kMergeThreads),
+                           pre, hs, p);
         if ((e = hipGetLastError()) != hipSuccess)
             return hip_fail(e, "chunk merge launch");
     }
