@@ -21,7 +21,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kRowBlock = 32;      // rows of a matrix-core tile
 constexpr int kChunkWaves = 8;
 constexpr int kStages = 4;         // KV tiles in LDS: one in use, the others on their way
-constexpr int kTileRows = kChunkWaves * kRowBlock;
+static_assert(kTileRows == kChunkWaves * kRowBlock, "a row block per wavefront");
 constexpr float kTiny = 1.17549435e-38f;   // the smallest normal float32
 constexpr float kLowest = -3.0e38f;       // the reference of a row without a score yet
 constexpr int kTilePages = kKeyTile / kPage;
@@ -60,10 +60,11 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
     s.L = (int)min((int64_t)max(ld_meta(p.ctx_lens, b), 0), (int64_t)p.max_pages * kPage);
     s.c.P = max(s.L - s.c.Q, 0);
     s.c.TT = p.TT;
+    s.c.G = p.G;
     return s;
 }
 
-// KV tiles of one head up to the end of each sequence, in s_end[0 .. B - 1].
+// Places of one head up to the end of each sequence, in s_end[0 .. B - 1].
 __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
     if (threadIdx.x < kWave) {
         const int lane = threadIdx.x;
@@ -87,22 +88,24 @@ __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
 struct Piece {
     int b, g, m;       // sequence, KV head, row tile
     int j0, j1;        // KV tiles [j0, j1) of it
-    int n;             // KV tiles of the whole unit
+    int n, weight;     // KV tiles of the whole unit, and places of each
     bool whole;
-    int64_t us;        // global index of the unit's first KV tile
-    int64_t next;
+    int64_t us;        // global index of the unit's first place
+    int64_t next;      // and of the first one behind the piece
 };
 
-// Ends a piece of unit r.us, r.m that starts at tile j0: with the unit, or with the range.
-__device__ __forceinline__ void cut_piece(Piece &r, const ChunkSeq &c, int64_t range_end) {
-    r.n = c.cost(r.m);
-    const int64_t unit_end = r.us + r.n + kUnitTiles;
+// The tiles of unit r.us, r.m (of sequence c) in places [from, range_end).
+__device__ __forceinline__ void cut_piece(Piece &r, const ChunkSeq &c, int64_t from, int64_t range_end) {
+    r.n = first_lane_int(c.cost(r.m));
+    r.weight = first_lane_int(c.weight(r.m));
+    const int64_t unit_end = r.us + (int64_t)r.n * r.weight + kUnitPlaces;
     r.next = unit_end < range_end ? unit_end : range_end;
-    r.j1 = first_lane_int(min((int)(r.next - r.us), r.n));   // (not above j0 in the places without tiles)
+    r.j0 = first_lane_int(min(tile_at(from - r.us, r.weight), r.n));
+    r.j1 = first_lane_int(min(tile_at(r.next - r.us, r.weight), r.n));
     r.whole = r.j0 == 0 && r.j1 == r.n;
 }
 
-// The unit that holds global tile x, and the part of it in [x, range_end).
+// The unit that holds place x, and the part of it in [x, range_end).
 // Units are laid out sequence by sequence, head by head, row tile by row tile.
 __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end, int64_t x, int64_t range_end) {
     const int lane = threadIdx.x & (kWave - 1);
@@ -136,8 +139,7 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end,
     r.m = first_lane_int(m);
     const int64_t start = c.before(r.m);
     r.us = x - in_head + start;
-    r.j0 = first_lane_int((int)(in_head - start));
-    cut_piece(r, c, range_end);
+    cut_piece(r, c, x, range_end);
     return r;
 }
 
@@ -146,14 +148,13 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end,
 // head follow each other, so most of the time nothing is searched.
 __device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t *s_end, int64_t &x, int64_t range_end, bool started, Piece &r) {
     while (x < range_end) {
-        const ChunkSeq c = started ? seq_info(p, r.b).c : ChunkSeq{0, 0, 1};
+        const ChunkSeq c = started ? seq_info(p, r.b).c : ChunkSeq{0, 0, 1, 1};
         if (started && (r.m + 1 < c.tiles() || r.g + 1 < p.Hkv)) {
             const bool same = r.m + 1 < c.tiles();
             r.g = same ? r.g : r.g + 1;
             r.m = same ? r.m + 1 : 0;
-            r.j0 = 0;
             r.us = x;
-            cut_piece(r, c, range_end);
+            cut_piece(r, c, x, range_end);
         } else {
             r = locate_tile(p, s_end, x, range_end);
         }
@@ -526,7 +527,7 @@ struct Chunk {
         Piece pc;
         if (!next_piece(p, s_end, x, end, false, pc))
             return;
-        bool first = pc.us + pc.j0 == begin;   // the range starts with it: its partial result's slot
+        bool first = pc.us <= begin;   // the range starts inside it: its partial result's slot
         State st;
         set_addresses(st, lds, wave, lane);
         Pages pages = start(p, st, pc, lds, wave, lane);
@@ -683,48 +684,70 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams 
     if (x >= ptot || x == prev)
         return;
     const Piece pc = locate_tile(p, s_tiles, x, ptot);
-    if (x == pc.us || x >= pc.us + pc.n || prev > pc.us)
+    if (x == pc.us || tile_at(x - pc.us, pc.weight) >= pc.n || prev > pc.us)
         return;   // no tiles are cut off here, or an earlier boundary cuts the unit too
-    const UnitSplit u = unit_split(ptot, pc.us, pc.n, p.W);
+    const int places = pc.n * pc.weight;
+    const UnitSplit u = unit_split(ptot, pc.us, places, p.W);
     const SeqInfo sq = seq_info(p, pc.b);
     constexpr int kPer = D / kMergeLanes;
     const int r = blockIdx.y * kMergeRows + threadIdx.x / kMergeLanes, part = threadIdx.x % kMergeLanes;
     const int token = pc.m * p.TT + r / p.G;
-    if (r >= p.TT * p.G || token >= sq.c.Q)
-        return;   // (whole rows of lanes)
-    const auto row_of = [&](int k) { return (int64_t)u.slot(k) * kTileRows + r; };
-    float M = -INFINITY;
-    for (int k = part; k < u.nparts; k += kMergeLanes)
-        M = fmaxf(M, p.ws_lse[row_of(k)]);
-#pragma unroll
-    for (int d = 1; d < kMergeLanes; d *= 2)
-        M = fmaxf(M, __shfl_xor(M, d, kWave));
-    float sum = 0.0f, o[kPer];
+    const bool row_ok = r < p.TT * p.G && token < sq.c.Q;   // (of whole rows of lanes)
+    if (__syncthreads_or(row_ok) == 0)
+        return;
+    __shared__ int s_slot[kMergeThreads];   // slots of up to 256 parts, -1: no tile starts among its places
+    float M = kLowest, sum = 0.0f, o[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; e++)
         o[e] = 0.0f;
-    for (int k0 = 0; k0 < u.nparts; k0 += kMergeAhead) {
-        f32x4_t v[kMergeAhead][kPer / 4];
-        float lse[kMergeAhead];
-#pragma unroll
-        for (int i = 0; i < kMergeAhead; i++) {
-            const int64_t row = row_of(min(k0 + i, u.nparts - 1));
-            lse[i] = p.ws_lse[row];
-#pragma unroll
-            for (int e = 0; e < kPer / 4; e++)
-                v[i][e] = *reinterpret_cast<const f32x4_t *>(p.ws_o + row * D + kPer * part + 4 * e);
+    for (int base = 0; base < u.nparts; base += kMergeThreads) {
+        const int n = min(u.nparts - base, kMergeThreads);
+        __syncthreads();
+        if ((int)threadIdx.x < n) {
+            const int k = base + threadIdx.x;
+            const int64_t lo = u.dense ? max(range_start(ptot, u.wlo + k, p.W, p.range_inv) - pc.us, (int64_t)0) : k;
+            const int64_t hi = u.dense ? min(range_start(ptot, u.wlo + k + 1, p.W, p.range_inv) - pc.us, (int64_t)places) : k + 1;
+            s_slot[threadIdx.x] = tile_at(lo, pc.weight) < tile_at(hi, pc.weight) ? u.slot(k) : -1;
         }
+        __syncthreads();
+        if (!row_ok)
+            continue;
+        for (int k0 = 0; k0 < n; k0 += kMergeAhead) {
+            f32x4_t v[kMergeAhead][kPer / 4];
+            float lse[kMergeAhead];
 #pragma unroll
-        for (int i = 0; i < kMergeAhead; i++) {
-            if (k0 + i >= u.nparts || lse[i] == -INFINITY)   // past the end, or a piece without a visible key
-                continue;
-            const float a = fmaxf(fast_exp2(lse[i] - M), kTiny);   // an infinite piece stays infinite
-            sum += a;
+            for (int i = 0; i < kMergeAhead; i++) {
+                const int slot = s_slot[min(k0 + i, n - 1)];
+                const int64_t row = (int64_t)max(slot, 0) * kTileRows + r;
+                lse[i] = slot < 0 || k0 + i >= n ? -INFINITY : p.ws_lse[row];
+#pragma unroll
+                for (int e = 0; e < kPer / 4; e++)
+                    v[i][e] = *reinterpret_cast<const f32x4_t *>(p.ws_o + row * D + kPer * part + 4 * e);
+            }
+            float m = M;
+#pragma unroll
+            for (int i = 0; i < kMergeAhead; i++)
+                m = fmaxf(m, lse[i]);
+            const float scale = fmaxf(fast_exp2(M - m), kTiny);   // (an infinite piece stays infinite)
+            M = m;
+            sum *= scale;
 #pragma unroll
             for (int e = 0; e < kPer; e++)
-                o[e] += a * v[i][e / 4][e % 4];
+                o[e] *= scale;
+#pragma unroll
+            for (int i = 0; i < kMergeAhead; i++) {
+                if (lse[i] == -INFINITY)   // no piece, or one without a visible key
+                    continue;
+                const float a = fmaxf(fast_exp2(lse[i] - M), kTiny);
+                sum += a;
+#pragma unroll
+                for (int e = 0; e < kPer; e++)
+                    o[e] += a * v[i][e / 4][e % 4];
+            }
         }
     }
+    if (!row_ok)
+        return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     uint16_t *dst = p.out + (int64_t)(sq.row0 + token) * p.out_stride + (int64_t)(pc.g * p.G + r % p.G) * D + kPer * part;
 #pragma unroll

@@ -5,10 +5,14 @@
 // A sequence of context length L with Q new tokens is cut into row tiles of TT
 // tokens.  Row tile j (from 0) ends at token min(Q, (j + 1) TT) and sees the
 // keys up to that token, so it takes ceil((P + min(Q, (j + 1) TT)) / 64) KV
-// tiles of 64 keys, P = max(L - Q, 0) (tokens in front of the chunk).  Its
-// share of the line of work is kUnitTiles longer: behind its KV tiles lie that
-// many places without any, so that workers with many short row tiles get
-// fewer KV tiles.
+// tiles of 64 keys, P = max(L - Q, 0) (tokens in front of the chunk).
+//
+// Workers share a line of places in equal ranges.  A KV tile has kTilePlaces
+// places where the row tile keeps most wavefronts busy, one where up to half of
+// its rows exist (that took about half as long), and belongs to the worker that
+// holds its first place; kUnitPlaces more at the end of each row tile have no KV
+// tile and stand for what starting and ending one costs, so that workers with
+// many short row tiles get fewer KV tiles.
 #pragma once
 
 #include <stdint.h>
@@ -18,7 +22,8 @@
 namespace tsattn {
 
 constexpr int kKeyTile = 64;   // keys per KV tile
-constexpr int kUnitTiles = 6;  // what starting and ending a row tile costs, in KV tiles
+constexpr int kTileRows = 256; // rows (tokens x query heads of a KV head) per row tile
+constexpr int kTilePlaces = 2, kUnitPlaces = 12;
 
 // sum over i = 0 .. n - 1 of floor((a i + b) / 64), for n <= 2^23, a <= 256:
 // whole multiples of 64 leave a and b, then the roles of the axes are swapped
@@ -49,22 +54,31 @@ struct ChunkSeq {
     int Q;      // new tokens
     int P;      // tokens in front of them
     int TT;     // tokens per row tile
+    int G;      // query heads per KV head
     TS_HOST_DEVICE int tiles() const { return (int)(((int64_t)Q + TT - 1) / TT); }
-    // KV tiles of row tile j
-    TS_HOST_DEVICE int keys_end(int j) const {
-        const int64_t e = (int64_t)(j + 1) * TT;
-        return P + (int)(e < Q ? e : Q);
+    // tokens of row tile j
+    TS_HOST_DEVICE int tokens(int j) const {
+        const int left = Q - j * TT;
+        return left < TT ? left : TT;
     }
-    TS_HOST_DEVICE int cost(int j) const { return (keys_end(j) + kKeyTile - 1) / kKeyTile; }
+    // KV tiles of row tile j
+    TS_HOST_DEVICE int cost(int j) const { return (P + j * TT + tokens(j) + kKeyTile - 1) / kKeyTile; }
+    // places of one of them
+    TS_HOST_DEVICE int weight(int j) const { return tokens(j) * G > kTileRows / 2 ? kTilePlaces : 1; }
     // places of row tiles 0 .. j - 1
     TS_HOST_DEVICE int64_t before(int j) const {
         const int full = Q / TT, n = j < full ? j : full;
-        int64_t c = floor_sum64((uint32_t)n, (uint32_t)TT, (uint64_t)P + TT + kKeyTile - 1);
+        int64_t c = 0;
+        if (n > 0)
+            c = weight(0) * floor_sum64((uint32_t)n, (uint32_t)TT, (uint64_t)P + TT + kKeyTile - 1);
         if (j > full)
-            c += cost(full);
-        return c + (int64_t)j * kUnitTiles;
+            c += (int64_t)weight(full) * cost(full);
+        return c + (int64_t)j * kUnitPlaces;
     }
     TS_HOST_DEVICE int64_t total() const { return before(tiles()); }
 };
+
+// First KV tile at or behind place `off` of a row tile.
+TS_HOST_DEVICE int tile_at(int64_t off, int weight) { return (int)((off + weight - 1) / weight); }
 
 }  // namespace tsattn

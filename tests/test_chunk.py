@@ -101,26 +101,37 @@ int main() {
     long n = 0;
     for (int it = 0; it < 20000; it++) {
         ChunkSeq s;
-        s.TT = 1 + rand() % 256;
+        s.G = 1 + rand() % 16;
+        s.TT = kTileRows / s.G;
         s.Q = 1 + rand() % (it % 2 ? 40 : 3000);
         s.P = rand() % (it % 3 ? 100 : 1000000);
         int64_t c = 0;
         int row = 0;
         for (int j = 0; j < s.tiles(); j++) {
-            if (s.before(j) != c) { printf("before(%d): Q %d P %d TT %d\n", j, s.Q, s.P, s.TT); return 1; }
+            if (s.before(j) != c) { printf("before(%d): Q %d P %d G %d\n", j, s.Q, s.P, s.G); return 1; }
             const int last = row + s.TT < s.Q ? row + s.TT : s.Q;   // tokens up to the tile's last
             int tiles = 0;
-            for (long t = 0; t < (long)s.P + last; t += 64) tiles++;
-            if (s.P < 5000 && tiles != s.cost(j)) { printf("cost(%d): Q %d P %d TT %d\n", j, s.Q, s.P, s.TT); return 1; }
-            c += s.cost(j) + kUnitTiles;
+            if (s.P < 5000) {
+                for (long t = 0; t < (long)s.P + last; t += 64) tiles++;
+                if (tiles != s.cost(j)) { printf("cost(%d): Q %d P %d G %d\n", j, s.Q, s.P, s.G); return 1; }
+            }
+            if (s.tokens(j) != last - row || s.weight(j) != ((last - row) * s.G > 128 ? 2 : 1)) return 2;
+            c += (int64_t)s.cost(j) * s.weight(j) + kUnitPlaces;
             row = last;
             n++;
         }
-        if (row != s.Q || s.total() != c) { printf("total: Q %d P %d TT %d\n", s.Q, s.P, s.TT); return 1; }
+        if (row != s.Q || s.total() != c) { printf("total: Q %d P %d G %d\n", s.Q, s.P, s.G); return 1; }
+        // a boundary anywhere in a row tile gives each KV tile to one side
+        const int w = s.weight(0), k = s.cost(0);
+        for (int off = 0; off <= k * w && off < 200; off++) {
+            int mine = 0;
+            for (int j = 0; j < k && j < 200; j++) mine += j * w < off;
+            if (tile_at(off, w) != mine) return 3;
+        }
     }
-    ChunkSeq s{1 << 22, 1 << 30, 8};   // the largest chunk behind the longest context
+    ChunkSeq s{1 << 22, 1 << 30, 16, 16};   // the largest chunk behind the longest context
     int64_t c = 0;
-    for (int j = 0; j < s.tiles(); j++) c += s.cost(j) + kUnitTiles;
+    for (int j = 0; j < s.tiles(); j++) c += (int64_t)s.cost(j) * s.weight(j) + kUnitPlaces;
     if (c != s.total()) return 1;
     printf("ok %ld\n", n);
     return 0;

@@ -277,3 +277,21 @@ def test_chunk_workspace_contents_do_not_matter():
     a = run_chunk(s).clone()
     b = run_chunk(s, workspace=ws).clone()
     assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_chunk_many_sequences_and_pieces():
+    """More sequences than one wavefront's lanes, empty ones among them; more
+    pieces of a unit than the merge holds at once; as many sequences as a call
+    takes."""
+    rng = np.random.default_rng(2)
+    q = rng.integers(0, 4, 300).tolist()
+    s = make(4, 2, 64, q, rng.integers(0, 90, 300).tolist(), seed=20)
+    check_chunk(s, "chunk 300 sequences", 0)
+    check_chunk(s, "chunk 300 sequences", 777)
+    s = make(2, 1, 64, [3], [40000], seed=21)
+    ref = reference(s)
+    for workers in (0, 500, 1300):
+        check_chunk(s, "chunk one unit in many pieces", workers, ref)
+    for D in (64, 128):
+        s = make(2, 1, D, [1] * 4096, [0] * 4096, seed=22)
+        check_chunk(s, f"chunk 4096 sequences, head_dim {D}", 0)
