@@ -70,7 +70,7 @@ constexpr int kLongSlice = 2;                    // passes of the longer slices
 constexpr int kBins = 256;
 constexpr double kBinsPerOctave = 8.0;
 constexpr int kMaxSlices = (1 << kMaxVocabBits) / kSliceUnit;
-constexpr int kPlanThreads = 256, kFilterThreads = 1024;
+constexpr int kPlanThreads = 1024, kFilterThreads = 1024;
 constexpr int kRun = 256;                        // logits that a wavefront reads at once of a whole row
 constexpr int kList = 8192;                      // candidates of a row
 constexpr int kFew = 256;                        // of them, compared pair by pair
@@ -88,6 +88,7 @@ struct RowPlan {
     float m;                // largest logit
     float lo, hi;
     bool by_count, then_p;  // a top-k ends among the candidates; then a top-p of what it keeps
+    bool summed;            // s_mass holds what is kept of each slice above the candidates
     u64 want;               // the running count or mass at which the filter ends (0: none does)
 };
 
@@ -378,10 +379,12 @@ struct DrawLds {
 struct PlanLds : DrawLds {
     u64 bin_mass[kBins];
     uint32_t bin_count[kBins];
+    int bins_off[kMaxSlices], shift[kMaxSlices];
 };
 struct FilterLds : DrawLds {
     u64 list[kList];        // ranks of the candidates
-    u64 digit[kDigits];     // sums by digit; of few candidates, their weights
+    u64 weight[kList];
+    u64 digit[kDigits];     // sums by digit
     u64 slice[kMaxSlices];  // kept mass of each slice
 };
 
@@ -615,6 +618,7 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
     Row r;
     r.b = blockIdx.x;
     const RowRule rule = row_rule(a, r.b);
+    const size_t slice0 = (size_t)r.b * a.slices;
     RowPlan plan;
     plan.state = kDrawn;
     if (draw_unfiltered<kPlanThreads>(a, rule, r, static_cast<const T *>(a.logits) + (int64_t)r.b * a.row_stride, s)) {
@@ -622,37 +626,53 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
             a.plan[r.b] = plan;
         return;
     }
-    static_assert(kBins == kPlanThreads, "one bin per thread");
     const double c = r.c, top = scaled(r.m, c);
     plan.state = kListed;
     plan.m = r.m;
     plan.lo = plan.hi = -FLT_MAX;
     plan.want = 0;
-    plan.by_count = plan.then_p = false;
+    plan.by_count = plan.then_p = plan.summed = false;
     plan.n = 0;
     if (rule.by_min)
         plan.lo = plan.hi = min_p_edge(rule, r.m);
     if (rule.by_k || rule.by_p) {
-        // the slices' bins on the row's grid
-        s.bin_count[tid] = 0;
-        s.bin_mass[tid] = 0;
-        __syncthreads();
-        const size_t slice0 = (size_t)r.b * a.slices;
-        const double top_bin = floor(top * kBinsPerOctave);
-        for (int i = 0; i < a.slices; i++) {
-            const uint32_t n = a.h_count[(slice0 + i) * kBins + tid];
-            const u64 mass = rule.by_p ? a.h_mass[(slice0 + i) * kBins + tid] : 0;
-            if (n == 0)
-                continue;
-            const double stop = scaled(a.s_max[slice0 + i], c);
-            const double off = top_bin - floor(stop * kBinsPerOctave), d = r.E - rint(stop);
-            const int at = (int)fmin(off + tid, (double)(kBins - 1));
-            atomicAdd(&s.bin_count[at], n);
-            if (d < 64.0)
-                atomicAdd(&s.bin_mass[at], mass >> (int)d);
+        // the slices' bins on the row's grid: a thread takes one bin of every
+        // kGroups-th slice
+        constexpr int kGroups = kPlanThreads / kBins, kAhead = 4;
+        const int own = tid % kBins, group = tid / kBins;
+        if (tid < kBins) {
+            s.bin_count[tid] = 0;
+            s.bin_mass[tid] = 0;
+        }
+        if (tid < a.slices) {   // how far a slice's grid and unit lie below the row's
+            const double stop = scaled(a.s_max[slice0 + tid], c);
+            s.bins_off[tid] = (int)fmin(floor(top * kBinsPerOctave) - floor(stop * kBinsPerOctave), (double)kBins);
+            s.shift[tid] = (int)fmin(r.E - rint(stop), 63.0);
         }
         __syncthreads();
-        const u64 count = s.bin_count[tid];
+        const double top_bin = floor(top * kBinsPerOctave);
+        for (int i0 = group; i0 < a.slices; i0 += kAhead * kGroups) {
+            uint32_t n[kAhead];
+            u64 mass[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const size_t at = (slice0 + min(i0 + k * kGroups, a.slices - 1)) * kBins + own;
+                n[k] = a.h_count[at];
+                mass[k] = rule.by_p ? a.h_mass[at] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const int i = i0 + k * kGroups;
+                if (i >= a.slices || n[k] == 0)
+                    continue;
+                const int at = min(s.bins_off[i] + own, kBins - 1);
+                atomicAdd(&s.bin_count[at], n[k]);
+                if (rule.by_p)
+                    atomicAdd(&s.bin_mass[at], mass[k] >> s.shift[i]);
+            }
+        }
+        __syncthreads();
+        const u64 count = tid < kBins ? s.bin_count[tid] : 0;
         u64 above, all, want, n_low, unused;
         int bin = kBins;   // the bin in which the first filter ends
         if (rule.by_k) {
@@ -677,6 +697,21 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
                 }
                 plan.state = !plan.then_p && s.bin_count[bin] <= kList ? kListed : kScanned;
             }
+            // What is kept anyway of each slice: where the bins hold masses and
+            // no min-p takes part, their sum above the last bin.
+            if (plan.state == kListed && rule.by_p && !rule.by_min) {
+                plan.summed = true;
+                const bool whole = plan.hi == INFINITY;
+                for (int i = tid / kWave; i < a.slices; i += kPlanThreads / kWave) {
+                    const int mine = whole ? 0 : bin - s.bins_off[i];   // bins of this slice that lie above it
+                    u64 sum = 0;
+                    for (int k = tid % kWave; k < mine; k += kWave)
+                        sum += a.h_mass[(slice0 + i) * kBins + k];
+                    sum = wave_incl_scan((uint64_t)sum);
+                    if (tid % kWave == kWave - 1)
+                        a.s_mass[slice0 + i] = sum >> s.shift[i];
+                }
+            }
         }
     }
     if (tid == 0)
@@ -697,6 +732,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
         return;
     const float lo = plan.lo, hi = plan.hi, m = plan.m;
     const size_t at_slice = (size_t)b * a.slices + slice;
+    const bool summed = plan.summed;
     if (a.s_max[at_slice] < lo) {   // nothing here
         if (tid == 0)
             a.s_mass[at_slice] = 0;
@@ -715,13 +751,15 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
 #pragma unroll
         for (int e = 0; e < kVec; e++) {
             mine += l[i][e] >= lo && l[i][e] < hi;
-            if (__any(l[i][e] >= hi))
+            if (!summed && __any(l[i][e] >= hi))
                 sum += l[i][e] >= hi && passes_min(rule, l[i][e], m) ? weight(scaled(l[i][e], rule.c), E) : 0;
         }
-    u64 total;
-    block_scan<kSliceThreads / kWave>(sum, waves, &total);
-    if (tid == 0)
-        a.s_mass[at_slice] = total;
+    if (!summed) {
+        u64 total;
+        block_scan<kSliceThreads / kWave>(sum, waves, &total);
+        if (tid == 0)
+            a.s_mass[at_slice] = total;
+    }
     u64 all;
     int at = (int)block_scan<kSliceThreads / kWave>((u64)mine, waves, &all) - mine;
     if (all == 0)
@@ -760,8 +798,6 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
     r.E = rint(scaled(r.m, r.c));
     const bool listed = plan.state == kListed;
     const int n_list = listed ? min(plan.n, a.list_len) : 0;
-    for (int i = tid; i < n_list; i += kFilterThreads)
-        s.list[i] = a.list[(size_t)r.b * a.list_len + i];
     if (tid < a.slices)
         s.slice[tid] = listed ? a.s_mass[slice0 + tid] : 0;
     __syncthreads();
@@ -771,15 +807,18 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
     constexpr int kIndex = (1 << kMaxVocabBits) - 1;
     const auto index_of = [](u64 rank) { return kIndex - (int)(rank & kIndex); };
     u64 all;
+    for (int i = tid; i < n_list; i += kFilterThreads) {
+        const u64 rank = a.list[(size_t)r.b * a.list_len + i];
+        s.list[i] = rank;
+        s.weight[i] = weight_of(logit_of(rank));
+    }
+    __syncthreads();
 
     if (listed && plan.hi == INFINITY && n_list <= kFew) {
         // Few logits in question: each thread compares its own with all the others.
-        u64 *w_of = s.digit;
+        u64 *w_of = s.weight;
         const bool mine = tid < n_list;
-        const u64 rank = mine ? s.list[tid] : 0, w = mine ? weight_of(logit_of(rank)) : 0;
-        if (mine)
-            w_of[tid] = w;
-        __syncthreads();
+        const u64 rank = mine ? s.list[tid] : 0, w = mine ? w_of[tid] : 0;
         u64 in_front = 0, mass_in_front = 0;
         if (mine)
             for (int j = 0; j < n_list; j++) {
@@ -833,21 +872,21 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
                 for (int i = tid; i < kDigits; i += kFilterThreads)
                     s.digit[i] = 0;
                 __syncthreads();
-                const auto take = [&](u64 rank, float l) {
+                const auto take = [&](u64 rank, auto weight) {
                     if (summing)
-                        kept += rank >= prefix ? weight_of(l) : 0;
+                        kept += rank >= prefix ? weight() : 0;
                     else if ((shift == 32 + kMaxVocabBits || rank >> shift == prefix) && rank >= floor_rank)
-                        atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight_of(l));
+                        atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight());
                 };
                 if (listed) {
                     for (int i = tid; i < n_list; i += kFilterThreads)
-                        take(s.list[i], logit_of(s.list[i]));
+                        take(s.list[i], [&] { return s.weight[i]; });
                 } else {
                     for_row(row, a.V, [&](int, const float(&l)[4], int at) {
 #pragma unroll
                         for (int e = 0; e < 4; e++)
                             if (l[e] >= plan.lo && l[e] < plan.hi)
-                                take(rank_of(l[e], at + e), l[e]);
+                                take(rank_of(l[e], at + e), [&] { return weight_of(l[e]); });
                     });
                 }
                 if (summing)
@@ -878,7 +917,7 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
             const u64 rank = s.list[i];
             const float l = logit_of(rank);
             if (rank >= cut && passes_min(rule, l, r.m))
-                atomicAdd(&s.slice[index_of(rank) / a.slice_len], weight_of(l));
+                atomicAdd(&s.slice[index_of(rank) / a.slice_len], s.weight[i]);
         }
     } else {
         for_row(row, a.V, [&](int run, const float(&l)[4], int at) {
