@@ -386,6 +386,9 @@ struct FilterLds : DrawLds {
     u64 weight[kList];
     u64 digit[kDigits];     // sums by digit
     u64 slice[kMaxSlices];  // kept mass of each slice
+    u64 few[kFew], few_weight[kFew];   // candidates that share the digits found so far
+    u64 differ, cut;
+    int n;
 };
 
 // First index i of the n values get(i) whose running sum reaches a target that
@@ -477,6 +480,15 @@ __device__ __forceinline__ void for_row(const T *row, int V, F f) {
             if (r0 + i * kWaves < runs)
                 f(r0 + i * kWaves, l[i], (r0 + i * kWaves) * kRun + 4 * lane);
     }
+}
+
+// Sum over kEach neighbouring lanes, in each of them.
+constexpr int kEach = kFilterThreads / kFew;
+__device__ __forceinline__ u64 sum_each(u64 x) {
+#pragma unroll
+    for (int d = 1; d < kEach; d *= 2)
+        x += __shfl_xor(x, d, kWave);
+    return x;
 }
 
 __device__ __forceinline__ float clamp_u(float u) { return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f; }
@@ -815,38 +827,42 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
     __syncthreads();
 
     if (listed && plan.hi == INFINITY && n_list <= kFew) {
-        // Few logits in question: each thread compares its own with all the others.
-        u64 *w_of = s.weight;
-        const bool mine = tid < n_list;
-        const u64 rank = mine ? s.list[tid] : 0, w = mine ? w_of[tid] : 0;
+        // Few logits in question: each is compared with all the others, by kEach
+        // neighbouring lanes.
+        const int own = tid / kEach, part = tid % kEach;
+        const bool mine = own < n_list;
+        const u64 rank = mine ? s.list[own] : 0, w = mine ? s.weight[own] : 0;
         u64 in_front = 0, mass_in_front = 0;
         if (mine)
-            for (int j = 0; j < n_list; j++) {
+            for (int j = part; j < n_list; j += kEach) {
                 const bool first = s.list[j] > rank;
                 in_front += first;
-                mass_in_front += first ? w_of[j] : 0;
+                mass_in_front += first ? s.weight[j] : 0;
             }
+        in_front = sum_each(in_front);
+        mass_in_front = sum_each(mass_in_front);
         bool kept = mine && !(plan.by_count && in_front >= (u64)rule.k);
         if (rule.by_p) {
             u64 want = plan.want;   // without top-k, of the whole row's mass
             if (plan.by_count) {
-                block_scan<kFilterThreads / kWave>(kept ? w : 0, s.waves, &all);
+                block_scan<kFilterThreads / kWave>(kept && part == 0 ? w : 0, s.waves, &all);
                 want = p_target(rule, all);
             }
             kept = kept && mass_in_front < want;
         }
         kept = kept && passes_min(rule, logit_of(rank), r.m);
         u64 Z;
-        block_scan<kFilterThreads / kWave>(kept ? w : 0, s.waves, &Z);   // (its barriers order the loops' reads)
-        if (mine)
-            w_of[tid] = kept ? w : 0;
+        block_scan<kFilterThreads / kWave>(kept && part == 0 ? w : 0, s.waves, &Z);   // (its barriers order the loops' reads)
+        if (mine && part == 0)
+            s.weight[own] = kept ? w : 0;
         __syncthreads();
         u64 target, unused, before = 0;
         fraction_of(r.u, Z, &target, &unused);
-        if (kept)
-            for (int j = 0; j < n_list; j++)
-                before += index_of(s.list[j]) < index_of(rank) ? w_of[j] : 0;
-        if (kept && before <= target && target < before + w)
+        if (kept)   // (the same for all lanes of a logit)
+            for (int j = part; j < n_list; j += kEach)
+                before += index_of(s.list[j]) < index_of(rank) ? s.weight[j] : 0;
+        before = sum_each(before);
+        if (kept && part == 0 && before <= target && target < before + w)
             write_token(a, r, index_of(rank), logit_of(rank), Z);
         return;
     }
@@ -854,43 +870,59 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
     u64 cut = 0;   // lowest rank that is kept
     if (plan.want) {
         // Finds the rank at which the running sum (of counts, or of weights) of
-        // the candidates reaches `want`, from its highest digit down; for a
-        // top-p of what a top-k keeps, once more with the weights.  Candidates
-        // that do not fit a list are read from the row.
+        // the candidates reaches `want`, from its highest digit down until few
+        // candidates share the digits found, which are compared pair by pair;
+        // for a top-p of what a top-k keeps, once more with the weights.
+        // Candidates that do not fit a list are read from the row.
+        const auto for_candidates = [&](auto f) {
+            if (listed) {
+                for (int i = tid; i < n_list; i += kFilterThreads)
+                    f(s.list[i], [&] { return s.weight[i]; });
+            } else {
+                for_row(row, a.V, [&](int, const float(&l)[4], int at) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (l[e] >= plan.lo && l[e] < plan.hi)
+                            f(rank_of(l[e], at + e), [&] { return weight_of(l[e]); });
+                });
+            }
+        };
+        // the highest bit in which candidates differ
+        int top = 32 + kMaxVocabBits;
+        u64 same = 0;
+        if (listed) {
+            if (tid == 0)
+                s.differ = 0;
+            __syncthreads();
+            same = s.list[0];
+            u64 differ = 0;
+            for (int i = tid; i < n_list; i += kFilterThreads)
+                differ |= s.list[i] ^ same;
+#pragma unroll
+            for (int d = 32; d; d >>= 1)
+                differ |= __shfl_xor(differ, d, kWave);
+            if (lane == 0 && differ)
+                atomicOr(&s.differ, differ);
+            __syncthreads();
+            top = s.differ ? 64 - __clzll((long long)s.differ) : 0;
+        }
         bool counts = plan.by_count;
         u64 want = plan.want;
         for (int round = 0; round <= (int)plan.then_p; round++) {
-            u64 prefix = 0;
+            u64 prefix = top < 64 ? same >> top : 0;
             const u64 floor_rank = cut;
-            u64 kept = 0;
-            for (int shift = 32 + kMaxVocabBits; shift >= 0;) {
-                // the last pass only sums the weights of what is kept
-                const bool summing = shift == 0;
-                if (summing && !(plan.then_p && round == 0))
-                    break;
+            int shift = top;
+            while (shift > 0) {
                 const int next = max(shift - kDigitBits, 0), digits = 1 << (shift - next);
                 for (int i = tid; i < kDigits; i += kFilterThreads)
                     s.digit[i] = 0;
+                if (tid == 0)
+                    s.n = 0;
                 __syncthreads();
-                const auto take = [&](u64 rank, auto weight) {
-                    if (summing)
-                        kept += rank >= prefix ? weight() : 0;
-                    else if ((shift == 32 + kMaxVocabBits || rank >> shift == prefix) && rank >= floor_rank)
+                for_candidates([&](u64 rank, auto weight) {
+                    if (rank >> shift == prefix && rank >= floor_rank)
                         atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight());
-                };
-                if (listed) {
-                    for (int i = tid; i < n_list; i += kFilterThreads)
-                        take(s.list[i], [&] { return s.weight[i]; });
-                } else {
-                    for_row(row, a.V, [&](int, const float(&l)[4], int at) {
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (l[e] >= plan.lo && l[e] < plan.hi)
-                                take(rank_of(l[e], at + e), [&] { return weight_of(l[e]); });
-                    });
-                }
-                if (summing)
-                    break;
+                });
                 __syncthreads();
                 u64 in_front, sum, goal;
                 // (a target past the sum, by rounding of the bins' masses, takes the last one)
@@ -901,9 +933,40 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
                 want = goal - in_front;
                 prefix = prefix << (shift - next) | (u64)(digits - 1 - d);
                 shift = next;
+                if (shift == 0)
+                    break;
+                for_candidates([&](u64 rank, auto weight) {
+                    if (rank >> shift == prefix && rank >= floor_rank) {
+                        const int i = atomicAdd(&s.n, 1);
+                        if (i < kFew) {
+                            s.few[i] = rank;
+                            s.few_weight[i] = counts ? 1 : weight();
+                        }
+                    }
+                });
+                if (tid == 0)
+                    s.cut = prefix << shift;   // (all of them, should rounding leave the target out of reach)
+                __syncthreads();
+                if (s.n <= kFew) {
+                    const int own = tid / kEach, n = s.n;
+                    const bool mine = own < n;
+                    u64 before = 0;
+                    if (mine)
+                        for (int j = tid % kEach; j < n; j += kEach)
+                            before += s.few[j] > s.few[own] ? s.few_weight[j] : 0;
+                    before = sum_each(before);
+                    if (mine && before < want && before + s.few_weight[own] >= want)
+                        s.cut = s.few[own];
+                    __syncthreads();
+                    prefix = s.cut;
+                    break;
+                }
+                __syncthreads();
             }
             cut = prefix;
             if (plan.then_p && round == 0) {
+                u64 kept = 0;
+                for_candidates([&](u64 rank, auto weight) { kept += rank >= cut ? weight() : 0; });
                 block_scan<kFilterThreads / kWave>(kept, s.waves, &all);
                 want = p_target(rule, all);
                 counts = false;
