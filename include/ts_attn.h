@@ -344,7 +344,8 @@ typedef struct ts_chunk_shape {
     int32_t num_kv_heads;       /* with 1 .. 16 query heads per KV head */
     int32_t head_dim;           /* 64 or 128 */
     int32_t page_size;          /* 16 */
-    int32_t max_q_len;          /* the longest chunk (upper bound), at most num_tokens */
+    int32_t max_q_len;          /* the longest chunk (upper bound), at most num_tokens; checked,
+                                   nothing is sized by it */
     int32_t max_pages_per_seq;  /* 1 .. 2^26 */
     int32_t max_ctx_len;        /* upper bound on ctx_lens; sizes the worker count only */
     int32_t num_workers;        /* 0: chosen by the library; the result does not depend on it
@@ -407,7 +408,7 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *   top-p (p < 1; else or NaN off)    of those, in descending order, each with
  *                                     less than p times their mass in front of
  *                                     it (the first one always);
- *   min-p (0 < m; capped at 1)        of those, the ones with w_v >= m.
+ *   min-p (0 < m; capped at 1; else or NaN off)  of those, the ones with w_v >= m.
  * Equal logits rank by index, the lowest first.  A temperature that is not
  * above 0 takes the largest logit.  logprob (may be NULL) is the natural
  * logarithm of the probability that the drawn token had among the kept ones (0
@@ -423,8 +424,9 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *   u            float32 [num_seqs], clamped to [0, 1 - 2^-24], NaN read as 0
  *   token        int32 [num_seqs];  logprob  float32 [num_seqs]
  * Asynchronous on `stream`; the workspace (ts_sample_workspace_size bytes,
- * 256-byte aligned, any contents) carries the slices' sums between the call's
- * two launches. */
+ * 256-byte aligned, any contents) carries the slices' sums and the candidates
+ * between the call's launches, two without filters (all three NULL) and four
+ * with them; calls that may run concurrently need distinct ones. */
 #define TS_LOGITS_F32 0
 #define TS_LOGITS_BF16 1
 

@@ -126,9 +126,9 @@ __device__ __forceinline__ RowRule row_rule(const SampleParams &a, int b) {
     r.by_k = !r.greedy && r.k > 0 && r.k < a.V;
     r.p = a.top_p ? a.top_p[b] : 1.0f;
     r.by_p = !r.greedy && r.p < 1.0f;
-    const float min_p = a.min_p ? fminf(a.min_p[b], 1.0f) : 0.0f;
-    r.by_min = !r.greedy && min_p > 0.0f;
-    r.min_x = r.by_min ? log2((double)min_p) : 0.0;
+    const float min_p = a.min_p ? a.min_p[b] : 0.0f;
+    r.by_min = !r.greedy && min_p > 0.0f;   // (not for NaN)
+    r.min_x = r.by_min ? log2((double)fminf(min_p, 1.0f)) : 0.0;
     return r;
 }
 

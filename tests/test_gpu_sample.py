@@ -143,6 +143,14 @@ def test_sample_unusable_logits_and_odd_parameters():
                 check(x, np.full(8, u, np.float32), f"unusable logits u {u} {f}", **{k: [v] * 8 for k, v in f.items()})
 
 
+def test_sample_min_p_nan_is_off():
+    nan = float("nan")
+    for V in (300, 20000):
+        x = logits_of(4, V, "float32", 17)
+        for u in (0.2, 0.99):
+            check(x, np.full(4, u, np.float32), f"min-p NaN V {V} u {u}", min_p=[nan, 0.5, nan, 0.0], top_k=[0, 0, 20, 20])
+
+
 def test_sample_strided_rows_and_no_log_probability():
     import torch
     from paper_2608_22788_amd import binding
