@@ -483,7 +483,7 @@ def _rows(t, name: str):
     """(tokens, heads, head_dim, row stride) of a packed token tensor, whose
     heads are contiguous."""
     shape, stride = t.shape, t.stride()
-    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or stride[1] != shape[2]:
+    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or stride[1] != shape[2] and shape[1] > 1:
         raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
     T, H, D = shape
     # the stride of a single row is never used; torch may report any value
