@@ -349,7 +349,8 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
                 const double bin = top_bin - floor(x * kBinsPerOctave);
                 const u64 w = rule.by_p ? weight(x, E) : 0;
                 if (bin < kBins - 1) {
-                    atomicAdd(&count_of[(int)bin], 1u);
+                    if (rule.by_k)
+                        atomicAdd(&count_of[(int)bin], 1u);
                     if (rule.by_p)
                         atomicAdd(&mass_of[(int)bin], w);
                 } else {
@@ -362,7 +363,8 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
     if (far_mass)
         atomicAdd(&mass_of[kBins - 1], far_mass);
     __syncthreads();
-    a.h_count[at_slice * kBins + tid] = count_of[tid];
+    if (rule.by_k)
+        a.h_count[at_slice * kBins + tid] = count_of[tid];
     if (rule.by_p)
         a.h_mass[at_slice * kBins + tid] = mass_of[tid];
 }
@@ -669,23 +671,36 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
 #pragma unroll
             for (int k = 0; k < kAhead; k++) {
                 const size_t at = (slice0 + min(i0 + k * kGroups, a.slices - 1)) * kBins + own;
-                n[k] = a.h_count[at];
+                n[k] = rule.by_k ? a.h_count[at] : 0;
                 mass[k] = rule.by_p ? a.h_mass[at] : 0;
             }
 #pragma unroll
             for (int k = 0; k < kAhead; k++) {
                 const int i = i0 + k * kGroups;
-                if (i >= a.slices || n[k] == 0)
+                if (i >= a.slices)
                     continue;
                 const int at = min(s.bins_off[i] + own, kBins - 1);
-                atomicAdd(&s.bin_count[at], n[k]);
-                if (rule.by_p)
+                if (n[k])
+                    atomicAdd(&s.bin_count[at], n[k]);
+                if (mass[k])
                     atomicAdd(&s.bin_mass[at], mass[k] >> s.shift[i]);
             }
         }
         __syncthreads();
-        const u64 count = tid < kBins ? s.bin_count[tid] : 0;
-        u64 above, all, want, n_low, unused;
+        // How many logits a bin holds: counted for top-k, else at most its mass
+        // over the weight at its lower edge, about a tenth too many (a weight
+        // is up to two units short, and each slice's sum was rounded down).
+        // The last bin has no lower edge and may hold any number.
+        u64 count = 0;
+        if (tid < kBins && rule.by_k) {
+            count = s.bin_count[tid];
+        } else if (tid < kBins - 1) {
+            const double least = exp2((top_bin - tid) / kBinsPerOctave - r.E + 42.0) - 2.0;   // 2^9 at least
+            count = s.bin_mass[tid] ? (u64)ceil((double)(s.bin_mass[tid] + (u64)a.slices) / least) : 0;
+        } else if (tid == kBins - 1) {
+            count = (u64)a.V;
+        }
+        u64 above, all, want, n_low, n_bin, unused;
         int bin = kBins;   // the bin in which the first filter ends
         if (rule.by_k) {
             bin = first_reaching<kPlanThreads, 1>(s, kBins, &above, &all, &want, [&](int) { return count; },
@@ -699,19 +714,25 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
         if (bin < kBins) {
             plan.then_p = plan.by_count && rule.by_p;
             first_reaching<kPlanThreads, 1>(s, bin + 1, &unused, &n_low, &unused, [&](int) { return count; }, [](u64) { return ~0ull; });
+            first_reaching<kPlanThreads, 1>(s, bin + 1, &unused, &n_bin, &unused, [&](int i) { return i == bin ? count : 0; },
+                                            [](u64) { return ~0ull; });
             plan.lo = bin_edge(top_bin, bin, c);
             plan.hi = INFINITY;
             plan.want = want;
-            if (n_low > kList) {
+            // Only the bin's own logits become candidates where all down to it
+            // are too many for the list, or too many to be compared pair by pair
+            // while the bins hold the mass of those above.
+            const bool sums = rule.by_p && !rule.by_min;
+            if (n_low > kList || (n_low > kFew && sums && !plan.then_p)) {
                 if (!plan.then_p) {
                     plan.hi = bin > 0 ? bin_edge(top_bin, bin - 1, c) : INFINITY;
                     plan.want = want - above;
                 }
-                plan.state = !plan.then_p && s.bin_count[bin] <= kList ? kListed : kScanned;
+                plan.state = !plan.then_p && n_bin <= kList ? kListed : kScanned;
             }
             // What is kept anyway of each slice: where the bins hold masses and
             // no min-p takes part, their sum above the last bin.
-            if (plan.state == kListed && rule.by_p && !rule.by_min) {
+            if (plan.state == kListed && sums) {
                 plan.summed = true;
                 const bool whole = plan.hi == INFINITY;
                 for (int i = tid / kWave; i < a.slices; i += kPlanThreads / kWave) {
@@ -913,28 +934,34 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
             const u64 floor_rank = cut;
             int shift = top;
             while (shift > 0) {
-                const int next = max(shift - kDigitBits, 0), digits = 1 << (shift - next);
-                for (int i = tid; i < kDigits; i += kFilterThreads)
-                    s.digit[i] = 0;
-                if (tid == 0)
-                    s.n = 0;
-                __syncthreads();
-                for_candidates([&](u64 rank, auto weight) {
-                    if (rank >> shift == prefix && rank >= floor_rank)
-                        atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight());
-                });
-                __syncthreads();
-                u64 in_front, sum, goal;
-                // (a target past the sum, by rounding of the bins' masses, takes the last one)
-                int d = first_reaching<kFilterThreads, kDigits / kFilterThreads>(
-                    s, digits, &in_front, &sum, &goal, [&](int i) { return s.digit[i]; },
-                    [&](u64 sum) { return want < sum ? want : sum; });
-                d = min(d, digits - 1);
-                want = goal - in_front;
-                prefix = prefix << (shift - next) | (u64)(digits - 1 - d);
-                shift = next;
-                if (shift == 0)
-                    break;
+                if (!listed || n_list > kFew) {
+                    const int next = max(shift - kDigitBits, 0), digits = 1 << (shift - next);
+                    for (int i = tid; i < kDigits; i += kFilterThreads)
+                        s.digit[i] = 0;
+                    if (tid == 0)
+                        s.n = 0;
+                    __syncthreads();
+                    for_candidates([&](u64 rank, auto weight) {
+                        if (rank >> shift == prefix && rank >= floor_rank)
+                            atomicAdd(&s.digit[digits - 1 - ((rank >> next) & (digits - 1))], counts ? 1ull : weight());
+                    });
+                    __syncthreads();
+                    u64 in_front, sum, goal;
+                    // (a target past the sum, by rounding of the bins' masses, takes the last one)
+                    int d = first_reaching<kFilterThreads, kDigits / kFilterThreads>(
+                        s, digits, &in_front, &sum, &goal, [&](int i) { return s.digit[i]; },
+                        [&](u64 sum) { return want < sum ? want : sum; });
+                    d = min(d, digits - 1);
+                    want = goal - in_front;
+                    prefix = prefix << (shift - next) | (u64)(digits - 1 - d);
+                    shift = next;
+                    if (shift == 0)
+                        break;
+                } else {
+                    if (tid == 0)
+                        s.n = 0;
+                    __syncthreads();
+                }
                 for_candidates([&](u64 rank, auto weight) {
                     if (rank >> shift == prefix && rank >= floor_rank) {
                         const int i = atomicAdd(&s.n, 1);
@@ -945,7 +972,7 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
                     }
                 });
                 if (tid == 0)
-                    s.cut = prefix << shift;   // (all of them, should rounding leave the target out of reach)
+                    s.cut = max(prefix << shift, floor_rank);   // (all of them, should rounding leave the target out of reach)
                 __syncthreads();
                 if (s.n <= kFew) {
                     const int own = tid / kEach, n = s.n;
