@@ -341,23 +341,33 @@ __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(SamplePara
     uint32_t far = 0;   // what lies in the last bin, most logits of a confident row, is summed in registers
     u64 far_mass = 0;
 #pragma unroll
-    for (int i = 0; i < kLoads; i++)
+    for (int i = 0; i < kLoads; i++) {
+        // (no branch per logit, so that the weights' chains run beside each other)
+        int bin[kVec];
+        u64 w[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; e++)
-            if (l[i][e] > -INFINITY) {
-                const double x = scaled(l[i][e], rule.c);
-                const double bin = top_bin - floor(x * kBinsPerOctave);
-                const u64 w = rule.by_p ? weight(x, E) : 0;
-                if (bin < kBins - 1) {
-                    if (rule.by_k)
-                        atomicAdd(&count_of[(int)bin], 1u);
-                    if (rule.by_p)
-                        atomicAdd(&mass_of[(int)bin], w);
-                } else {
-                    far++;
-                    far_mass += w;
-                }
+            bin[e] = (int)fmin(top_bin - floor(scaled(l[i][e], rule.c) * kBinsPerOctave), kBins - 1.0);
+        if (rule.by_p) {
+#pragma unroll
+            for (int e = 0; e < kVec; e++) {
+                w[e] = weight(scaled(l[i][e], rule.c), E);
+                far_mass += bin[e] == kBins - 1 ? w[e] : 0;
             }
+#pragma unroll
+            for (int e = 0; e < kVec; e++)
+                if (bin[e] < kBins - 1)
+                    atomicAdd(&mass_of[bin[e]], w[e]);
+        }
+        if (rule.by_k) {
+#pragma unroll
+            for (int e = 0; e < kVec; e++) {
+                far += bin[e] == kBins - 1 && l[i][e] > -INFINITY;
+                if (bin[e] < kBins - 1)
+                    atomicAdd(&count_of[bin[e]], 1u);
+            }
+        }
+    }
     if (far)
         atomicAdd(&count_of[kBins - 1], far);
     if (far_mass)
