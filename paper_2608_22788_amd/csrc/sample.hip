@@ -768,6 +768,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
     constexpr int kVec = 16 / sizeof(T), kLoads = 16 * kPasses / kVec;
     __shared__ u64 waves[kSliceThreads / kWave];
     __shared__ int at_list;
+    __shared__ float dense[kSliceUnit];
     const int b = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
     const int tid = threadIdx.x;
     const RowPlan &plan = a.plan[b];
@@ -775,7 +776,6 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
         return;
     const float lo = plan.lo, hi = plan.hi, m = plan.m;
     const size_t at_slice = (size_t)b * a.slices + slice;
-    const bool summed = plan.summed;
     if (a.s_max[at_slice] < lo) {   // nothing here
         if (tid == 0)
             a.s_mass[at_slice] = 0;
@@ -786,20 +786,44 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
     const T *src = static_cast<const T *>(a.logits) + (int64_t)b * a.row_stride + first;
     float l[kLoads][kVec];
     load_slice<T, kPasses>(src, n, l);
-    const double E = rint(scaled(m, rule.c));
-    u64 sum = 0;
     int mine = 0;
 #pragma unroll
     for (int i = 0; i < kLoads; i++)
 #pragma unroll
-        for (int e = 0; e < kVec; e++) {
+        for (int e = 0; e < kVec; e++)
             mine += l[i][e] >= lo && l[i][e] < hi;
-            if (!summed && __any(l[i][e] >= hi))
-                sum += l[i][e] >= hi && passes_min(rule, l[i][e], m) ? weight(scaled(l[i][e], rule.c), E) : 0;
+    if (!plan.summed) {
+        u64 total = 0;
+        if (hi < INFINITY) {
+            // The logits to be summed are put side by side first, a pass at a
+            // time: a weight costs a wavefront the same for one lane as for all
+            // (a min-p that keeps 5 % took 39 us in place).
+            const double E = rint(scaled(m, rule.c));
+            u64 sum = 0;
+#pragma unroll
+            for (int pass = 0; pass < kPasses; pass++) {
+                int kept = 0;
+#pragma unroll
+                for (int i = pass * kLoads / kPasses; i < (pass + 1) * kLoads / kPasses; i++)
+#pragma unroll
+                    for (int e = 0; e < kVec; e++)
+                        kept += l[i][e] >= hi;
+                u64 n;   // (the scan's barriers end the reads of the pass before)
+                int at = (int)block_scan<kSliceThreads / kWave>((u64)kept, waves, &n) - kept;
+                if (kept) {
+#pragma unroll
+                    for (int i = pass * kLoads / kPasses; i < (pass + 1) * kLoads / kPasses; i++)
+#pragma unroll
+                        for (int e = 0; e < kVec; e++)
+                            if (l[i][e] >= hi)
+                                dense[at++] = l[i][e];
+                }
+                __syncthreads();
+                for (int i = tid; i < (int)n; i += kSliceThreads)
+                    sum += passes_min(rule, dense[i], m) ? weight(scaled(dense[i], rule.c), E) : 0;
+            }
+            block_scan<kSliceThreads / kWave>(sum, waves, &total);
         }
-    if (!summed) {
-        u64 total;
-        block_scan<kSliceThreads / kWave>(sum, waves, &total);
         if (tid == 0)
             a.s_mass[at_slice] = total;
     }
@@ -811,6 +835,8 @@ __global__ __launch_bounds__(kSliceThreads) void sample_gather_kernel(SamplePara
         at_list = atomicAdd(&a.plan[b].n, (int)all);
     __syncthreads();
     at += at_list;
+    if (mine == 0)
+        return;
 #pragma unroll
     for (int i = 0; i < kLoads; i++)
 #pragma unroll
@@ -1013,11 +1039,20 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
 
     // the kept mass of every slice, and the draw
     if (listed) {
-        for (int i = tid; i < n_list; i += kFilterThreads) {
-            const u64 rank = s.list[i];
-            const float l = logit_of(rank);
-            if (rank >= cut && passes_min(rule, l, r.m))
-                atomicAdd(&s.slice[index_of(rank) / a.slice_len], s.weight[i]);
+        // (a slice's candidates are neighbours in the list: most wavefronts have
+        // one slice, whose sum takes one addition in place of 64 to one address)
+        for (int i0 = 0; i0 < n_list; i0 += kFilterThreads) {
+            const int i = i0 + tid;
+            const u64 rank = s.list[min(i, n_list - 1)];
+            const u64 w = i < n_list && rank >= cut && passes_min(rule, logit_of(rank), r.m) ? s.weight[i] : 0;
+            const int slice = index_of(rank) / a.slice_len;
+            if (__all(slice == first_lane_int(slice))) {
+                const u64 sum = wave_incl_scan((uint64_t)w);
+                if (lane == kWave - 1 && sum)
+                    atomicAdd(&s.slice[slice], sum);
+            } else if (w) {
+                atomicAdd(&s.slice[slice], w);
+            }
         }
     } else {
         for_row(row, a.V, [&](int run, const float(&l)[4], int at) {
