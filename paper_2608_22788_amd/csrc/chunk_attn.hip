@@ -36,6 +36,7 @@ struct ChunkParams {
     uint16_t *out;
     float *ws_o;                // [2W][kTileRows][D] partial outputs, normalised
     float *ws_lse;              // [2W][kTileRows] log2-sum-exp
+    struct Cut *cuts;           // [W] the unit at the start of each worker's range
     int64_t q_stride, out_stride, num_pages;
     int B, Hq, Hkv, G, max_pages, num_tokens;
     int TT;                     // tokens per row tile
@@ -97,6 +98,16 @@ __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
     __syncthreads();
 }
 
+// What joins the pieces of the unit that holds the first place of a worker's
+// range, as chunk_merge_kernel needs it (which took 16.7 us for 32 mixed
+// sequences when it searched the unit itself, so 8.6).
+struct Cut {
+    int64_t ptot, us;  // places of the call, and in front of the unit
+    int n, weight;     // KV tiles of the unit, and places of each
+    int row, tokens;   // its first packed row, and its tokens
+    int head;          // and first query head
+};
+
 struct Piece {
     int b, g, m;       // sequence, KV head, row tile
     int j0, j1;        // KV tiles [j0, j1) of it
@@ -156,12 +167,12 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end,
 }
 
 // The next piece with KV tiles at or behind x in a worker's range, false if
-// there is none.  `r` is the piece before it, if `started`: the row tiles of one
-// head follow each other, so most of the time nothing is searched.
-__device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t *s_end, int64_t &x, int64_t range_end, bool started, Piece &r) {
+// there is none.  `r` is the piece before it, whether it has tiles or not: the
+// row tiles of one head follow each other, so most of the time nothing is searched.
+__device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t *s_end, int64_t &x, int64_t range_end, Piece &r) {
     while (x < range_end) {
-        const ChunkSeq c = started ? seq_info(p, r.b).c : ChunkSeq{0, 0, 1, 1};
-        if (started && (r.m + 1 < c.tiles() || r.g + 1 < p.Hkv)) {
+        const ChunkSeq c = seq_info(p, r.b).c;
+        if (r.m + 1 < c.tiles() || r.g + 1 < p.Hkv) {
             const bool same = r.m + 1 < c.tiles();
             r.g = same ? r.g : r.g + 1;
             r.m = same ? r.m + 1 : 0;
@@ -170,7 +181,6 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t 
         } else {
             r = locate_tile(p, s_end, x, range_end);
         }
-        started = true;
         x = r.next;
         if (r.j0 < r.j1)
             return true;
@@ -535,9 +545,16 @@ struct Chunk {
         const int wave = first_lane_int(threadIdx.x / kWave);
         const int h = lane >> 5;
         const int r = wave * kRowBlock + (lane & 31);
-        int64_t x = begin;
-        Piece pc;
-        if (!next_piece(p, s_end, x, end, false, pc))
+        if (begin >= end)
+            return;
+        Piece pc = locate_tile(p, s_end, begin, end);
+        int64_t x = pc.next;
+        if (threadIdx.x == 0) {
+            const SeqInfo sq = seq_info(p, pc.b);
+            const int at = pc.m * p.TT;
+            p.cuts[w] = Cut{(int64_t)s_end[p.B - 1] * p.Hkv, pc.us, pc.n, pc.weight, sq.row0 + at, min(p.TT, sq.c.Q - at), pc.g * p.G};
+        }
+        if (pc.j0 >= pc.j1 && !next_piece(p, s_end, x, end, pc))
             return;
         bool first = pc.us <= begin;   // the range starts inside it: its partial result's slot
         State st;
@@ -620,7 +637,7 @@ struct Chunk {
                     add_odd(p, st, p.page_table + (size_t)pc.b * p.max_pages, pc.g, plain * kKeyTile, min(pc.j1 * kKeyTile, sq.L), h);
             }
             Piece nx = pc;
-            const bool more = next_piece(p, s_end, x, end, true, nx);
+            const bool more = next_piece(p, s_end, x, end, nx);
             if (more)
                 pages = start(p, st, nx, lds, wave, lane);
             if (row_ok)
@@ -673,6 +690,8 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(Chun
     const int w = xcd_worker(blockIdx.x, p.W);
     const int64_t begin = first_lane_int64(range_start(ptot, w, p.W, p.range_inv));
     const int64_t end = first_lane_int64(range_start(ptot, w + 1, p.W, p.range_inv));
+    if (ptot == 0 && w == p.W - 1 && threadIdx.x == 0)
+        p.cuts[w].ptot = 0;
     Chunk<D>::work(p, s_tiles, w, begin, end, lds);
 }
 
@@ -687,25 +706,25 @@ constexpr int merge_rows(int D) { return kMergeThreads / (D / 8); }
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams p) {
     constexpr int kMergeRows = merge_rows(D), kMergeLanes = D / 8;
-    extern __shared__ uint64_t s_tiles[];
-    tile_ends(p, s_tiles);
-    const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
     const int w = blockIdx.x + 1;
-    const int64_t x = first_lane_int64(range_start(ptot, w, p.W, p.range_inv));
-    const int64_t prev = first_lane_int64(range_start(ptot, w - 1, p.W, p.range_inv));
+    Cut cut = p.cuts[w];
+    const int64_t ptot = p.cuts[p.W - 1].ptot;   // (that range is never empty)
+    if (ptot == 0)
+        return;
+    const int64_t x = range_start(ptot, w, p.W, p.range_inv);
+    const int64_t prev = range_start(ptot, w - 1, p.W, p.range_inv);
     if (x >= ptot || x == prev)
         return;
-    const Piece pc = locate_tile(p, s_tiles, x, ptot);
-    if (x == pc.us || tile_at(x - pc.us, pc.weight) >= pc.n || prev > pc.us)
+    if (ptot < p.W)   // some ranges are empty, w's maybe
+        cut = p.cuts[worker_of(ptot, x, p.W)];
+    if (x == cut.us || tile_at(x - cut.us, cut.weight) >= cut.n || prev > cut.us)
         return;   // no tiles are cut off here, or an earlier boundary cuts the unit too
-    const int places = pc.n * pc.weight;
-    const UnitSplit u = unit_split(ptot, pc.us, places, p.W);
-    const SeqInfo sq = seq_info(p, pc.b);
+    const int places = cut.n * cut.weight;
+    const UnitSplit u = unit_split(ptot, cut.us, places, p.W);
     constexpr int kPer = D / kMergeLanes;
     const int r = blockIdx.y * kMergeRows + threadIdx.x / kMergeLanes, part = threadIdx.x % kMergeLanes;
-    const int token = pc.m * p.TT + r / p.G;
-    const bool row_ok = r < p.TT * p.G && token < sq.c.Q;   // (of whole rows of lanes)
-    if (__syncthreads_or(row_ok) == 0)
+    const bool row_ok = r < cut.tokens * p.G;   // (of whole rows of lanes)
+    if (blockIdx.y * kMergeRows >= cut.tokens * p.G)
         return;
     __shared__ int s_slot[kMergeThreads];   // slots of up to 256 parts, -1: no tile starts among its places
     float M = kLowest, sum = 0.0f, o[kPer];
@@ -717,9 +736,9 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams 
         __syncthreads();
         if ((int)threadIdx.x < n) {
             const int k = base + threadIdx.x;
-            const int64_t lo = u.dense ? max(range_start(ptot, u.wlo + k, p.W, p.range_inv) - pc.us, (int64_t)0) : k;
-            const int64_t hi = u.dense ? min(range_start(ptot, u.wlo + k + 1, p.W, p.range_inv) - pc.us, (int64_t)places) : k + 1;
-            s_slot[threadIdx.x] = tile_at(lo, pc.weight) < tile_at(hi, pc.weight) ? u.slot(k) : -1;
+            const int64_t lo = u.dense ? max(range_start(ptot, u.wlo + k, p.W, p.range_inv) - cut.us, (int64_t)0) : k;
+            const int64_t hi = u.dense ? min(range_start(ptot, u.wlo + k + 1, p.W, p.range_inv) - cut.us, (int64_t)places) : k + 1;
+            s_slot[threadIdx.x] = tile_at(lo, cut.weight) < tile_at(hi, cut.weight) ? u.slot(k) : -1;
         }
         __syncthreads();
         if (!row_ok)
@@ -761,7 +780,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams 
     if (!row_ok)
         return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *dst = p.out + (int64_t)(sq.row0 + token) * p.out_stride + (int64_t)(pc.g * p.G + r % p.G) * D + kPer * part;
+    uint16_t *dst = p.out + (int64_t)(cut.row + r / p.G) * p.out_stride + (int64_t)(cut.head + r % p.G) * D + kPer * part;
 #pragma unroll
     for (int e = 0; e < kPer; e += 4)
         *reinterpret_cast<uint2 *>(dst + e) =
@@ -770,7 +789,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkParams 
 
 struct ChunkPlan {
     int G, TT, W;
-    size_t ws_lse_off, ws_bytes;
+    size_t ws_lse_off, ws_cut_off, ws_bytes;
 };
 
 int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
@@ -785,7 +804,8 @@ int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
     pl->W = s->num_workers > 0 ? s->num_workers : (int)std::max<int64_t>(1, std::min<int64_t>(256, tiles / 2));
     const size_t rows = 2 * (size_t)pl->W * kTileRows;
     pl->ws_lse_off = rows * s->head_dim * sizeof(float);
-    pl->ws_bytes = (pl->ws_lse_off + rows * sizeof(float) + 255) & ~(size_t)255;
+    pl->ws_cut_off = pl->ws_lse_off + rows * sizeof(float);
+    pl->ws_bytes = (pl->ws_cut_off + pl->W * sizeof(Cut) + 255) & ~(size_t)255;
     return TS_OK;
 }
 
@@ -874,6 +894,7 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     p.out = static_cast<uint16_t *>(out);
     p.ws_o = static_cast<float *>(workspace);
     p.ws_lse = reinterpret_cast<float *>(static_cast<char *>(workspace) + pl.ws_lse_off);
+    p.cuts = reinterpret_cast<Cut *>(static_cast<char *>(workspace) + pl.ws_cut_off);
     p.q_stride = q_stride;
     p.out_stride = out_stride;
     p.num_pages = s->num_pages;
@@ -902,7 +923,7 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
         return hip_fail(e, "chunk attention launch");
     if (pl.W > 1) {
         hipLaunchKernelGGL(merge_k, dim3((unsigned)pl.W - 1, kTileRows / merge_rows(s->head_dim)), dim3(kMergeThreads),
-                           pre, hs, p);
+                           0, hs, p);
         if ((e = hipGetLastError()) != hipSuccess)
             return hip_fail(e, "chunk merge launch");
     }
