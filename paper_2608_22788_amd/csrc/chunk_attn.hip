@@ -1,4 +1,47 @@
-// chunk_attn.hip -- attention of chunks of new tokens over the paged cache.
+// chunk_attn.hip -- attention of chunks of new tokens over the paged cache: any
+// number of packed rows per sequence, from one decoding token to a whole prompt.
+//
+// For row i of a sequence (Q new tokens, context length L) and query head h:
+//   out = sum_t w_t V_t / sum_t w_t,  w_t = exp(scale <q, K_t>),  t <= L - Q + i.
+// In one pass over the keys, in units of log2: with a reference m that is at
+// least the largest score so far less 8, w_t = 2^(s_t - m); where a score passes
+// m + 8, m moves up to it and what is summed so far is scaled by 2^(old - new).
+// Weights stay below 2^8, sums are float32, and a weight is rounded to bf16 for
+// the second matrix product only (as the decoding kernels do).
+//
+// Work.  A row tile is 256 rows of one KV head (256 / G tokens with their G query
+// heads each, so that a key is read once for the group), a KV tile 64 keys.  A
+// workgroup of 8 wavefronts, one per CU, holds 32 rows per wavefront: q, the
+// running sums and the output in registers.  The KV tiles of all row tiles form
+// one line that is cut into W equal ranges (chunk_partition.h), so a ragged batch
+// and a causal prompt load all CUs alike whatever their lengths; a row tile that
+// a boundary cuts leaves its pieces, normalised, with their log2-sum-exp in the
+// workspace, and chunk_merge_kernel joins them.
+//
+// Scores are computed transposed, S^T = K Q^T (32 x 32 x 16 products), so that
+// a lane holds scores of one row and its weights are already where the second
+// product O^T += V^T P^T takes them from; V^T is read by the transposing LDS
+// read.  Tiles come to LDS by loads that pass no registers, four stages deep, and
+// rows are stored in an order without bank conflicts (measured: none).
+//
+// What bounds it.  Long chunks: 4 D operations per row and key.  At 8,192 tokens
+// of a prompt, 32/8 heads, head_dim 128: 521 us, 1,055 TFLOP/s, 77 % of what a
+// 16384^3 bf16 product reaches on the card (533 us on another box).  The clock
+// falls to 2.0-2.2 GHz; of a SIMD's cycles the matrix unit is busy 54 %, and
+// other vector instructions (an exponential, a multiply-add, a sum, a maximum and
+// half a packing for each score) issue in 36 %.  What mattered, on that case:
+//   - 128 rows on 4 wavefronts took 781 us: every CU then draws 10 TB/s of tiles
+//     through the L2s, which alone take 423 us; 256 rows halve that;
+//   - a tile's weights beside the next tile's scores, in a fixed order: 551 us
+//     (577 in the order that the compiler chose);
+//   - no effect: wave priorities, operands read six products ahead instead of
+//     four; two wavefronts to the halves of one tile: 564 instead of 555.
+// head_dim 64 has twice the exponentials per operation: 94 us at 56.9 GFLOP.
+// Long caches under few rows: the cache's bytes, 16 KiB of K and as much of V per
+// tile.  32 sequences, most of them decoding behind up to 4,000 tokens: 81 us for
+// 317 MB; 256 sequences of one token behind 1,000: 199 us for 1,057 MB, 5.3 TB/s.
+// One short chunk (37 tokens behind 2,011, 23 us): the chain of a launch, finding
+// the work, two tiles and the join of 16 pieces.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
