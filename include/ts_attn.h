@@ -387,8 +387,9 @@ int ts_rope_append(const ts_chunk_shape *shape, const ts_rope_config *cfg, const
  * sequence,
  *   out[r][h][:] = sum_t softmax_t(scale * <q[r][h][:], K_t>) V_t,
  *   t in [0, L_b - Q_b + i].
- * Rows that see no key (Q_b > L_b) get zeros.  Keys and values that a row does
- * not see do not enter its result, also where they are infinite or NaN.
+ * Rows that see no key (positions below 0, where Q_b > L_b) get zeros.  out may
+ * be q itself (with the same stride).  Keys and values that a row does not see
+ * do not enter its result, also where they are infinite or NaN.
  * `workspace` is device memory of at least ts_chunk_attn_workspace_size bytes,
  * 256-byte aligned, with any contents; calls that may run concurrently need
  * distinct ones. */

@@ -581,7 +581,10 @@ struct Chunk {
         return pages;
     }
 
-    // A worker's range.  While a piece's result is written, the first tiles of
+    // A worker's range.  A row's query is read by the workers of its row tile
+    // alone, and output is written after it: by the one that has the whole tile,
+    // or by the merge kernel (so the output may take the queries' place).
+    // While a piece's result is written, the first tiles of
     // the next one are already on their way.
     __device__ __forceinline__ static void work(const ChunkParams &p, const uint64_t *s_end, int w, int64_t begin, int64_t end, char *lds) {
         const int lane = threadIdx.x & (kWave - 1);
@@ -925,6 +928,8 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     const int64_t row = (int64_t)s->num_q_heads * s->head_dim;
     if ((st = check_stride("q_stride", q_stride, row)) || (st = check_stride("out_stride", out_stride, row)))
         return st;
+    if (out == q && out_stride != q_stride)
+        return fail(TS_ERR_ARG, "out == q needs equal strides");
     if ((st = check_device()))
         return st;
     ChunkParams p;

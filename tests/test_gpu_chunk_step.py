@@ -2,6 +2,8 @@
 attention over the cache, the draw of the next token -- against the float64
 oracles, captured into a graph, on two streams, with a cache past 4 GiB, and
 next to the library's decode attention."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -172,6 +174,19 @@ def test_chunk_agrees_with_decode_attention():
         assert (x - y).abs().max().item() <= 0.05 and ((x - y).norm() / y.norm()).item() <= 1e-2
 
 
+def test_chunk_output_in_place_of_the_queries():
+    import torch
+    from paper_2608_22788_amd import binding
+    for W in (0, 1, 7, 1000):
+        s = make(8, 2, 128, [200, 1, 90, 16], [700, 30, 0, 5000], seed=9)
+        out = torch.zeros(s["q"].shape, dtype=torch.bfloat16, device="cuda")
+        say("in place, workers", W)
+        binding.chunk_attn(s["q"], s["k_pages"], s["v_pages"], s["table"], s["ctx"], s["starts"], out, s["scale"], num_workers=W)
+        n = int(s["starts"][-1])
+        binding.chunk_attn(s["q"], s["k_pages"], s["v_pages"], s["table"], s["ctx"], s["starts"], s["q"], s["scale"], num_workers=W)
+        assert torch.equal(s["q"][:n].view(torch.int16), out[:n].view(torch.int16))
+
+
 def test_cache_past_4_gib():
     """Pages whose byte offset needs more than 32 bits, read and written."""
     import torch
@@ -217,6 +232,12 @@ def test_empty_calls_and_refusals_of_the_binding():
     assert err.value.status == -3
     with pytest.raises(binding.TsError):
         binding.chunk_attn(**good, scale=float("nan"))
+    wide = torch.zeros(s["q"].shape[0], 16, 64, dtype=torch.bfloat16, device="cuda")
+    shape = binding.chunk_shape_of(s["q"], s["k_pages"], s["table"])
+    ws = torch.empty(binding.chunk_workspace_size(shape), dtype=torch.uint8, device="cuda")
+    args = [ctypes.byref(shape), wide.data_ptr(), 512, s["k_pages"].data_ptr(), s["v_pages"].data_ptr(), s["table"].data_ptr(),
+            s["ctx"].data_ptr(), s["starts"].data_ptr(), wide.data_ptr(), 1024, 1.0, ws.data_ptr(), ws.numel(), None]
+    assert binding.lib.ts_chunk_attn(*args) == -6                 # in place with two strides
     with pytest.raises(binding.TsError):
         binding.chunk_attn(**good, scale=1.0, max_q_len=6)        # above the number of rows
     torch.cuda.synchronize()

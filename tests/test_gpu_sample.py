@@ -143,6 +143,30 @@ def test_sample_unusable_logits_and_odd_parameters():
                 check(x, np.full(8, u, np.float32), f"unusable logits u {u} {f}", **{k: [v] * 8 for k, v in f.items()})
 
 
+def test_sample_the_longest_row():
+    V = 1 << 20
+    for name in ("none", "k40", "k_many", "p", "m", "kpm"):
+        x = logits_of(2, V, "bfloat16", 23, holes=False)
+        check(x, np.array([0.4, 0.999], np.float32), f"sample V {V} {name}", temperature=[1.0, 3.0],
+              **{k: [v] * 2 for k, v in FILTERS[name].items()})
+
+
+def test_sample_the_most_rows():
+    """65,536 rows, every 64th the same: the draws repeat with them."""
+    import torch
+    x = logits_of(64, 50, "float32", 29)
+    u = torch.linspace(0, 0.99, 64, device="cuda")
+    f = dict(top_k=torch.arange(64, device="cuda").int() % 7, top_p=0.4 + 0.01 * torch.arange(64, device="cuda"))
+    lists = {k: v.tolist() for k, v in f.items()}
+    check(x, u.cpu().numpy(), "64 of 65,536 rows", **lists)
+    want = torch.tensor(draw(x, u.cpu().numpy(), **lists)[0], device="cuda")
+    from paper_2608_22788_amd import binding
+    token = torch.zeros(65536, dtype=torch.int32, device="cuda")
+    say("65,536 rows")
+    binding.sample(x.repeat(1024, 1), u.repeat(1024), token, **{k: v.repeat(1024) for k, v in f.items()})
+    assert torch.equal(token.view(1024, 64), want.view(1, 64).expand(1024, 64))
+
+
 def test_sample_min_p_nan_is_off():
     nan = float("nan")
     for V in (300, 20000):
