@@ -38,8 +38,8 @@
 //     four; two wavefronts to the halves of one tile: 564 instead of 555.
 // head_dim 64 has twice the exponentials per operation: 94 us at 56.9 GFLOP.
 // Long caches under few rows: the cache's bytes, 16 KiB of K and as much of V per
-// tile.  32 sequences, most of them decoding behind up to 4,000 tokens: 81 us for
-// 317 MB; 256 sequences of one token behind 1,000: 199 us for 1,057 MB, 5.3 TB/s.
+// tile.  32 sequences, most of them decoding behind up to 4,000 tokens: 77 us for
+// 317 MB; 256 sequences of one token behind 1,000: 183 us for 1,057 MB, 5.8 TB/s.
 // One short chunk (37 tokens behind 2,011, 23 us): the chain of a launch, finding
 // the work, two tiles and the join of 16 pieces.
 #include <hip/hip_runtime.h>
@@ -256,22 +256,31 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 // for written before it is; m0, which they need, has no other use in these
 // kernels.  Completion is counted by vmcnt: dma_wait() and a barrier come before
 // the data is read.
-template <int kLoads>
+//
+// Keys that one row tile alone reads (kOnce) are loaded as not to be kept: 256
+// sequences of one token behind 1,000 take 181 us so, 198 otherwise; a prompt,
+// whose row tiles find each other's keys in the L2, would take 588 instead of 519.
+template <int kLoads, bool kOnce>
 __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int from, int twist) {
     static_assert(kLoads == 2 || kLoads == 4, "blocks");
-    if constexpr (kLoads == 4)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                     "buffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
-                     "buffer_load_dwordx4 %3, %1, 0 offen offset:1024 lds\n\t"
-                     "buffer_load_dwordx4 %4, %1, 0 offen offset:2048 lds\n\t"
-                     "buffer_load_dwordx4 %5, %1, 0 offen offset:%6 lds"
-                     ::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist), "v"(from ^ 2 * twist), "v"(from ^ 3 * twist), "n"(3 * 1024)
-                     : "memory");
-    else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-                     "buffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
-                     "buffer_load_dwordx4 %3, %1, 0 offen offset:1024 lds"
-                     ::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist) : "memory");
+#define TS_DMA_BLOCK(reg, offset, kept) "buffer_load_dwordx4 %" reg ", %1, 0 offen offset:" offset kept " lds\n\t"
+#define TS_DMA_BLOCKS(kept)                                                                                            \
+    if constexpr (kLoads == 4)                                                                                         \
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept) TS_DMA_BLOCK("3", "1024", kept)    \
+                         TS_DMA_BLOCK("4", "2048", kept) TS_DMA_BLOCK("5", "%6", kept)::"s"(to), "s"(rsrc), "v"(from), \
+                     "v"(from ^ twist), "v"(from ^ 2 * twist), "v"(from ^ 3 * twist), "n"(3 * 1024)                    \
+                     : "memory");                                                                                      \
+    else                                                                                                               \
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept)                                   \
+                         TS_DMA_BLOCK("3", "1024", kept)::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist)             \
+                     : "memory")
+    if constexpr (kOnce) {
+        TS_DMA_BLOCKS(" nt");
+    } else {
+        TS_DMA_BLOCKS("");
+    }
+#undef TS_DMA_BLOCKS
+#undef TS_DMA_BLOCK
 }
 // Waits until at most the loads of the last `later` tiles are under way.
 template <int kLoads>
@@ -318,7 +327,7 @@ struct Chunk {
     // Starts loading a wavefront's part of a tile, the keys (wavefronts 0 to 3)
     // or values of a page.  A page outside the pool is stored as zeros; what is
     // under way then arrives first, so that counts of loads stay counts of tiles.
-    __device__ __forceinline__ static void dma_page(const ChunkParams &p, const State &st, int pid, int g, char *stage, int wave, int lane) {
+    __device__ __forceinline__ static void dma_page(const ChunkParams &p, const State &st, int pid, bool once, int g, char *stage, int wave, int lane) {
         char *to = stage + wave * (kPage * kRowBytes);   // (the values follow the keys)
         if (__builtin_expect(pid < 0 || pid >= p.num_pages, 0)) {
             dma_wait<kLoads>(0);
@@ -329,7 +338,11 @@ struct Chunk {
         }
         const size_t base = ((size_t)pid * p.Hkv + g) * (size_t)(kPage * D);
         const block_rsrc_t rsrc = block_rsrc((wave < kTilePages ? p.k_pages : p.v_pages) + base, kPage * kRowBytes);
-        dma_blocks<kLoads>(rsrc, first_lane_int((int)(uintptr_t)(lds_char *)to), st.from, st.twist);
+        const uint32_t at = (uint32_t)first_lane_int((int)(uintptr_t)(lds_char *)to);
+        if (once)
+            dma_blocks<kLoads, true>(rsrc, at, st.from, st.twist);
+        else
+            dma_blocks<kLoads, false>(rsrc, at, st.from, st.twist);
     }
 
     __device__ __forceinline__ static void set_addresses(State &st, char *lds, int wave, int lane) {
@@ -559,6 +572,7 @@ struct Chunk {
     struct Pages {
         const int32_t *pt;
         int first, last;   // page of the first tile; the last page of the context
+        bool once;         // no other row tile reads them
         int ids[4];
         __device__ __forceinline__ int next(int i) {   // tiles i = 0, 1, ... of the piece, in order
             if (i % 4 == 0)
@@ -574,10 +588,10 @@ struct Chunk {
     __device__ __forceinline__ static Pages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
         const SeqInfo sq = seq_info(p, pc.b);
         Pages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
-                    first_lane_int((max(sq.L, 1) - 1) / kPage), {}};
+                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}};
         const int n = min(pc.j1 - pc.j0, kStages - 1);
         for (int i = 0; i < n; i++)
-            dma_page(p, st, pages.next(i), pc.g, lds + i * kStage, wave, lane);
+            dma_page(p, st, pages.next(i), pages.once, pc.g, lds + i * kStage, wave, lane);
         return pages;
     }
 
@@ -644,7 +658,7 @@ struct Chunk {
             const auto advance = [&](int i) __attribute__((always_inline)) {
                 arrive(i + 1, min(n - 2 - i, 1));
                 if (i + kStages - 1 < n)
-                    dma_page(p, st, pages.next(i + kStages - 1), pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
+                    dma_page(p, st, pages.next(i + kStages - 1), pages.once, pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
             const auto step = [&](int i, Scores &c, Scores &next) __attribute__((always_inline)) {
                 advance(i);
