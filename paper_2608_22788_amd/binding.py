@@ -479,22 +479,27 @@ def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, 
 # The smallest of these calls run for less than Python takes to check their
 # arguments attribute by attribute, so each attribute is read once.
 
+_BF16, _I32 = torch.bfloat16, torch.int32
+
+
 def _rows(t, name: str):
     """(tokens, heads, head_dim, row stride) of a packed token tensor, whose
     heads are contiguous."""
-    shape, stride = t.shape, t.stride()
-    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or stride[1] != shape[2] and shape[1] > 1:
-        raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
-    T, H, D = shape
-    # the stride of a single row is never used; torch may report any value
-    return T, H, D, stride[0] if T > 1 else H * D
+    if t.dtype is _BF16 and t.dim() == 3:
+        T, H, D = t.shape
+        if t.is_contiguous():
+            return T, H, D, H * D
+        row, head, value = t.stride()
+        if value == 1 and (head == D or H == 1):
+            # the stride of a single row is never used; torch may report any value
+            return T, H, D, row if T > 1 else H * D
+    raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
 
 
 def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts):
     """(num_pages, kv_heads, page size, head_dim, sequences, pages per sequence)."""
-    bf16, i32 = torch.bfloat16, torch.int32
-    if (k_pages.dtype != bf16 or v_pages.dtype != bf16 or page_table.dtype != i32 or ctx_lens.dtype != i32 or
-            q_starts.dtype != i32):
+    if not (k_pages.dtype is _BF16 and v_pages.dtype is _BF16 and page_table.dtype is _I32 and ctx_lens.dtype is _I32 and
+            q_starts.dtype is _I32):
         raise ValueError("k_pages and v_pages must be bf16, page_table, ctx_lens and q_starts int32 tensors")
     if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous() and
             ctx_lens.is_contiguous() and q_starts.is_contiguous()):
