@@ -39,12 +39,12 @@
 //     the list (pair by pair if few, else by a radix descent over (logit,
 //     index)) and draws.
 // Measured, 151,936 logits a row: 8 float32 rows with temperature alone 12.4
-// us; 200 bf16 rows, each with its own filters, 96 us (kernels 41, 11, 23 and 25
+// us; 200 bf16 rows, each with its own filters, 94 us (kernels 42, 10, 20 and 25
 // us; with one workgroup reading each filtered row again instead of the last
 // two kernels' slices it was 245 us).  200 rows, every one with top-k 50: 59-64
 // us, top-p 0.9: 95-107, min-p 0.05: 42-55, none: 41, of which the weights'
 // arithmetic is the largest part (slices 34; reading them alone 12.6).  48
-// float32 rows of 50,257 with top-p: 42 us, the chain of four launches.  Only a
+// float32 rows of 50,257 with top-p: 41 us, the chain of four launches.  Only a
 // row of which more than kList logits lie in one bin is still read by one
 // workgroup.
 #include <hip/hip_runtime.h>
@@ -396,6 +396,7 @@ struct PlanLds : DrawLds {
     u64 bin_mass[kBins];
     uint32_t bin_count[kBins];
     int bins_off[kMaxSlices], shift[kMaxSlices];
+    u64 n_low, n_bin;
 };
 struct FilterLds : DrawLds {
     u64 list[kList];        // ranks of the candidates
@@ -714,7 +715,7 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
         } else if (tid == kBins - 1) {
             count = (u64)a.V;
         }
-        u64 above, all, want, n_low, n_bin, unused;
+        u64 above, all, want, unused;
         int bin = kBins;   // the bin in which the first filter ends
         if (rule.by_k) {
             bin = first_reaching<kPlanThreads, 1>(s, kBins, &above, &all, &want, [&](int) { return count; },
@@ -727,9 +728,14 @@ __global__ __launch_bounds__(kPlanThreads) void sample_plan_kernel(SampleParams 
                       kBins - 1);
         if (bin < kBins) {
             plan.then_p = plan.by_count && rule.by_p;
-            first_reaching<kPlanThreads, 1>(s, bin + 1, &unused, &n_low, &unused, [&](int) { return count; }, [](u64) { return ~0ull; });
-            first_reaching<kPlanThreads, 1>(s, bin + 1, &unused, &n_bin, &unused, [&](int i) { return i == bin ? count : 0; },
-                                            [](u64) { return ~0ull; });
+            // logits down to the bin, and in it (thread bin holds both)
+            const u64 down_to = block_scan<kPlanThreads / kWave>(count, s.waves, &unused);
+            if (tid == bin) {
+                s.n_low = down_to;
+                s.n_bin = count;
+            }
+            __syncthreads();
+            const u64 n_low = s.n_low, n_bin = s.n_bin;
             plan.lo = bin_edge(top_bin, bin, c);
             plan.hi = INFINITY;
             plan.want = want;

@@ -151,6 +151,34 @@ def test_two_streams_with_their_own_workspaces():
             assert torch.equal(s["out"].view(torch.int16), out.view(torch.int16)) and torch.equal(s["token"], token)
 
 
+def test_workspace_of_another_call():
+    """Calls with few tiles, or none at all, that take over the workspace of a
+    larger one, and one full of ones."""
+    import torch
+    from paper_2608_22788_amd import binding
+    big = make(8, 2, 128, [500, 60, 1], [3000, 100, 2000], seed=10)
+    small = make(8, 2, 128, [3, 0, 1], [0, 0, 90], seed=11)
+    W = 100
+    shape = binding.chunk_shape_of(big["q"], big["k_pages"], big["table"], num_workers=W)
+    ws = torch.full((binding.chunk_workspace_size(shape),), 1, dtype=torch.uint8, device="cuda")
+
+    def run(s, starts):
+        out = torch.full(s["q"].shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        binding.chunk_attn(s["q"], s["k_pages"], s["v_pages"], s["table"], s["ctx"], starts, out, s["scale"], workspace=ws,
+                           num_workers=W)
+        torch.cuda.synchronize()
+        return out.view(torch.int16)
+
+    say("no rows, workspace of ones")
+    assert (run(small, torch.zeros_like(small["starts"])).view(torch.bfloat16) == 7.0).all()
+    first = run(small, small["starts"])
+    say("after a larger call")
+    run(big, big["starts"])
+    assert torch.equal(run(small, small["starts"]), first)
+    run(big, big["starts"])
+    assert (run(small, torch.zeros_like(small["starts"])).view(torch.bfloat16) == 7.0).all()
+
+
 def test_chunk_agrees_with_decode_attention():
     """Up to 16 new tokens a sequence both kernels compute the same attention:
     they differ by the rounding of either (each within the bound of its tests)."""
