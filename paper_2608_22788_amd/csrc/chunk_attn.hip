@@ -453,8 +453,7 @@ struct Chunk {
                 x[half][e] = fast_exp2(__builtin_fmaf(c.s[half][e], p.scale_log2, -st.m_ref));
                 if (e % 2) {
                     pf[half][e / 8][e / 2 % 4] = pack_bf16x2(x[half][e - 1], x[half][e]);
-                    sum[0] += x[half][e - 1];
-                    sum[1] += x[half][e];
+                    sum[e / 2 % 2] = dot2_bf16(pf[half][e / 8][e / 2 % 4], 0x3f803f80u, sum[e / 2 % 2]);
                 }
             }
             asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));   // (here, not at the end of the step: 1.7 %)
