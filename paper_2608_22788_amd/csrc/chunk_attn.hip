@@ -6,8 +6,9 @@
 // In one pass over the keys, in units of log2: with a reference m that is at
 // least the largest score so far less 8, w_t = 2^(s_t - m); where a score passes
 // m + 8, m moves up to it and what is summed so far is scaled by 2^(old - new).
-// Weights stay below 2^8, sums are float32, and a weight is rounded to bf16 for
-// the second matrix product only (as the decoding kernels do).
+// Weights stay at 2^8 or below; they are rounded to bf16 for the second matrix
+// product, which takes no more, and their float32 sum takes the rounded ones too,
+// so that the result stays an average of values (two to an instruction).
 //
 // Work.  A row tile is 256 rows of one KV head (256 / G tokens with their G query
 // heads each, so that a key is read once for the group), a KV tile 64 keys.  A
@@ -28,15 +29,17 @@
 // of a prompt, 32/8 heads, head_dim 128: 521 us, 1,055 TFLOP/s, 77 % of what a
 // 16384^3 bf16 product reaches on the card (533 us on another box).  The clock
 // falls to 2.0-2.2 GHz; of a SIMD's cycles the matrix unit is busy 54 %, and
-// other vector instructions (an exponential, a multiply-add, a sum, a maximum and
-// half a packing for each score) issue in 36 %.  What mattered, on that case:
+// other vector instructions (an exponential, a multiply-add and half a maximum, a
+// packing and a sum for each score) issue in 36 %.  What mattered, on that case:
 //   - 128 rows on 4 wavefronts took 781 us: every CU then draws 10 TB/s of tiles
 //     through the L2s, which alone take 423 us; 256 rows halve that;
 //   - a tile's weights beside the next tile's scores, in a fixed order: 551 us
 //     (577 in the order that the compiler chose);
-//   - no effect: wave priorities, operands read six products ahead instead of
-//     four; two wavefronts to the halves of one tile: 564 instead of 555.
-// head_dim 64 has twice the exponentials per operation: 94 us at 56.9 GFLOP.
+//   - weights summed two at a time: 428 -> 423 us with four resumed rollouts;
+//   - no effect: more of the weights beside the scores, wave priorities, operands
+//     read six products ahead instead of four; worse: two wavefronts to the halves
+//     of one tile (564 instead of 555), 64 rows per wavefront (726 instead of 522).
+// head_dim 64 has twice the exponentials per operation: 92 us for 56.9 GFLOP.
 // Long caches under few rows: the cache's bytes, 16 KiB of K and as much of V per
 // tile.  32 sequences, most of them decoding behind up to 4,000 tokens: 77 us for
 // 317 MB; 256 sequences of one token behind 1,000: 183 us for 1,057 MB, 5.8 TB/s.
