@@ -219,6 +219,17 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _own_workspace(nbytes: int, device, stream, zeros: bool = False):
+    """The workspace of a call that was given none, made on the stream that the
+    call runs on: the allocator hands memory out again in the order of the stream
+    it was made for, so nobody else uses it before the call or, once the caller
+    drops it, during the call."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):   # another library's, with its handle
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream), device=device)
+    with torch.cuda.stream(stream):   # (None: the current one stays)
+        return (torch.zeros if zeros else torch.empty)(nbytes, dtype=torch.uint8, device=device)
+
+
 def shape_of(q, k_pages, page_table, max_ctx_len=None, num_workers=0, variant=0) -> AttnShape:
     B, Qmax, Hq, D = q.shape
     NP, Hkv, P, D2 = k_pages.shape
@@ -250,7 +261,8 @@ def new_workspace(nbytes: int, device="cuda"):
 def decode_attn(q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale: float,
                 workspace=None, max_ctx_len: Optional[int] = None, num_workers: int = 0,
                 stream=None, events=None, variant: int = 0):
-    """ts_decode_attn on torch tensors; returns the workspace tensor used.
+    """ts_decode_attn on torch tensors; returns the workspace tensor used (without
+    one it is made on the call's stream, here as in the calls below).
 
     ``events`` = (begin, end) handles from ``Event`` to time the main kernel.
     """
@@ -259,7 +271,7 @@ def decode_attn(q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale: f
     shape = shape_of(q, k_pages, page_table, max_ctx_len, num_workers, variant)
     need = workspace_size(shape)
     if workspace is None:
-        workspace = new_workspace(need, q.device)
+        workspace = _own_workspace(need, q.device, stream, zeros=True)
     elif workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes, "
                          f"this call needs {need}")
@@ -460,12 +472,11 @@ def kv_append(k_new, v_new, k_pages, v_pages, page_table, ctx_lens, q_lens, stre
 def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, num_accepted, next_token,
                 workspace=None, stream=None):
     """ts_spec_accept on torch tensors; returns the workspace used."""
-    import torch
     B, G1, V = p_target.shape
     G = G1 - 1
     need = int(lib.ts_spec_accept_workspace_size(B, V))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=p_target.device)
+        workspace = _own_workspace(need, p_target.device, stream)
     ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
     check(lib.ts_spec_accept(B, V, G, p_target.data_ptr(), ptr(q_draft), ptr(draft_tokens),
                              num_draft.data_ptr(), ptr(u_accept), u_sample.data_ptr(), num_accepted.data_ptr(),
@@ -584,7 +595,7 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
     shape = ChunkShape(B, T, Hq, Hkv, D, P, T if max_q_len is None else int(max_q_len), maxp,
                        maxp * P if max_ctx_len is None else int(max_ctx_len), num_workers, NP)
     if workspace is None:
-        workspace = torch.empty(chunk_workspace_size(shape), dtype=torch.uint8, device=q.device)
+        workspace = _own_workspace(chunk_workspace_size(shape), q.device, stream)
     check(lib.ts_chunk_attn(ctypes.byref(shape), q.data_ptr(), q_stride, k_pages.data_ptr(), v_pages.data_ptr(),
                             page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
                             out_stride, scale, workspace.data_ptr(),
@@ -617,7 +628,7 @@ def sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=N
             raise ValueError(f"{name} must be a contiguous {dt} vector with a value per row")
     _check_device(logits, u, token, logprob, temperature, top_k, top_p, min_p, workspace)
     if workspace is None:
-        workspace = torch.empty(sample_workspace_size(B, V), dtype=torch.uint8, device=logits.device)
+        workspace = _own_workspace(sample_workspace_size(B, V), logits.device, stream)
     check(lib.ts_sample(B, V, LOGITS_F32 if logits.dtype == torch.float32 else LOGITS_BF16, logits.data_ptr(),
                         logits.stride(0) if B > 1 else V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                         u.data_ptr(), token.data_ptr(), _ptr(logprob), workspace.data_ptr(),
