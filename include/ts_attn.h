@@ -334,8 +334,9 @@ int ts_spec_accept(int32_t num_seqs, int32_t vocab, int32_t max_draft, const flo
  * are 16-byte aligned.  Pages, page table and lengths are those of
  * ts_decode_attn.  The calls are asynchronous on `stream`, allocate nothing
  * and read no device data on the host.  No array content makes them access
- * memory out of bounds: starts are clamped to [0, num_tokens], lengths to the
- * page table; a page id outside [0, num_pages) reads as zeros and is not
+ * memory out of bounds: starts are clamped to [0, num_tokens], lengths to
+ * [0, max_pages_per_seq x 16] (the rows' positions follow the clamped length, in
+ * both operators); a page id outside [0, num_pages) reads as zeros and is not
  * written. */
 typedef struct ts_chunk_shape {
     int32_t num_seqs;           /* 1 .. 4096 */
@@ -364,8 +365,8 @@ typedef struct ts_chunk_shape {
  *   k_pages[page_table[b][t / 16]][g][t % 16][:] = x for keys, and
  *   v_pages[...] = v[r][g][:] unchanged.
  * float32 throughout, angles reduced in float64, one rounding to bf16.
- * q_out may be q itself (with the same stride).  A row whose position or page
- * id falls outside the pool writes its query, but no key or value.
+ * q_out may be q itself (with the same stride).  A row in front of position 0,
+ * or whose page id falls outside the pool, writes its query, but no key or value.
  *   inv_freq        float32 [rot_dim / 2] (may be NULL if rot_dim is 0)
  *   q_norm, k_norm  bf16 [head_dim], or NULL: no norm
  * Uses every field of the shape but max_q_len, max_ctx_len and num_workers. */

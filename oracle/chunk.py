@@ -6,12 +6,17 @@ TEST INFRASTRUCTURE ONLY: the product library never uses this module, and
 nothing here is shared with it.
 
 Packed rows: sequence b owns rows starts[b] .. starts[b + 1] - 1, and ctx[b]
-counts them, so its row i is at position ctx[b] - Q + i.
+counts them, so its row i is at position ctx[b] - Q + i.  Starts are clamped to
+the rows, lengths to what the page table has room for, in both operators.
 """
 from __future__ import annotations
 
 
 import numpy as np
+
+
+def _length(ctx, b, table, page):
+    return min(max(int(ctx[b]), 0), table.shape[1] * page)
 
 
 def _owned(starts, b, rows):
@@ -42,7 +47,7 @@ def chunk_attention(q, k_pages, v_pages, table, ctx, starts, scale):
     out, mag = np.full((T, Hq, D), np.nan), np.full((T, Hq, D), np.nan)
     for b in range(len(ctx)):
         a, e = _owned(starts, b, T)
-        Q, L = e - a, int(ctx[b])
+        Q, L = e - a, _length(ctx, b, table, k_pages.shape[2])
         if Q == 0:
             continue
         last = np.arange(L - Q, L)                     # position of each row
@@ -94,9 +99,9 @@ def rope_append(q, k, v, k_pages, v_pages, table, ctx, starts, inv_freq, q_norm=
     for b in range(len(ctx)):
         a, e = _owned(starts, b, T)
         for r in range(a, e):
-            pos = int(ctx[b]) - (e - r)
+            pos = _length(ctx, b, table, P) - (e - r)
             q_out[r] = turn(q[r], q_norm, pos)
-            if pos < 0 or pos >= table.shape[1] * P:
+            if pos < 0:
                 continue
             pid = int(table[b][pos // P])
             if 0 <= pid < k_pages.shape[0]:

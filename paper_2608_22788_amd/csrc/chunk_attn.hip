@@ -104,7 +104,7 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
     const int e = min(max(ld_meta(p.q_starts, b + 1), 0), p.num_tokens);
     s.row0 = a;
     s.c.Q = max(e - a, 0);
-    s.L = (int)min((int64_t)max(ld_meta(p.ctx_lens, b), 0), (int64_t)p.max_pages * kPage);
+    s.L = clamped_len(ld_meta(p.ctx_lens, b), p.max_pages);
     s.c.P = max(s.L - s.c.Q, 0);
     s.c.TT = p.TT;
     s.c.G = p.G;

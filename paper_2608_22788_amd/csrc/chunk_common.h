@@ -31,4 +31,9 @@ __device__ __forceinline__ int find_packed_seq(const int32_t *q_starts, int B, i
     return first_lane_int(max(0, min(lo + __popcll(__ballot(before)), B - 1)));
 }
 
+// Context length as the operators take it: what the page table has room for.
+__device__ __forceinline__ int clamped_len(int len, int max_pages) {
+    return (int)min((int64_t)max(len, 0), (int64_t)max_pages * kPage);
+}
+
 }  // namespace tsattn

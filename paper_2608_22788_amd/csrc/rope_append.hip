@@ -109,10 +109,10 @@ __global__ __launch_bounds__(kRopeWaves * kWave) void rope_append_kernel(RopePar
             if (wave == 0) {
                 const int b = find_packed_seq(p.q_starts, p.B, (int)t);
                 const int first = ld_meta(p.q_starts, b), end = min(ld_meta(p.q_starts, b + 1), p.num_tokens);
-                const int64_t pos = (int64_t)ld_meta(p.ctx_lens, b) - (end - t);
+                const int64_t pos = clamped_len(ld_meta(p.ctx_lens, b), p.max_pages) - (end - t);
                 const bool used = first <= t && t < end;
                 int64_t slot = -1;
-                if (used && pos >= 0 && pos < (int64_t)p.max_pages * kPage) {
+                if (used && pos >= 0) {   // (below the clamped length, so inside the table)
                     const int page = ld_meta(p.page_table, (size_t)b * p.max_pages + pos / kPage);
                     if (page >= 0 && page < p.num_pages)
                         slot = (int64_t)page * p.Hkv * kPage + pos % kPage;
