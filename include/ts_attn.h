@@ -328,16 +328,16 @@ int ts_spec_accept(int32_t num_seqs, int32_t vocab, int32_t max_draft, const flo
  * tensors (Q_b of them; q_starts int32 [num_seqs + 1], not decreasing), and
  * ctx_lens[b] = L_b counts them: row i of a sequence is at position
  * L_b - Q_b + i.  Rows outside every sequence (behind q_starts[num_seqs]) are
- * neither read nor written.  A token tensor's row holds heads x head_dim
- * contiguous bf16 values, rows are `stride` elements apart (a multiple of 8,
- * so that q, k and v can be views of one projection's output), and pointers
- * are 16-byte aligned.  Pages, page table and lengths are those of
- * ts_decode_attn.  The calls are asynchronous on `stream`, allocate nothing
- * and read no device data on the host.  No array content makes them access
- * memory out of bounds: starts are clamped to [0, num_tokens], lengths to
- * [0, max_pages_per_seq x 16] (the rows' positions follow the clamped length, in
- * both operators); a page id outside [0, num_pages) reads as zeros and is not
- * written. */
+ * never written; they may be read, but what they hold enters no result.  A
+ * token tensor's row holds heads x head_dim contiguous bf16 values, rows are
+ * `stride` elements apart (a multiple of 8, so that q, k and v can be views of
+ * one projection's output), and pointers are 16-byte aligned.  Pages, page
+ * table and lengths are those of ts_decode_attn.  The calls are asynchronous on
+ * `stream`, allocate nothing and read no device data on the host.  No array
+ * content makes them access memory out of bounds: starts are clamped to
+ * [0, num_tokens], lengths to [0, max_pages_per_seq x 16] (the rows' positions
+ * follow the clamped length, in both operators); a page id outside
+ * [0, num_pages) reads as zeros and is not written. */
 typedef struct ts_chunk_shape {
     int32_t num_seqs;           /* 1 .. 4096 */
     int32_t num_tokens;         /* rows of the token tensors, 0 .. 2^22 */
