@@ -349,8 +349,9 @@ typedef struct ts_chunk_shape {
                                    nothing is sized by it */
     int32_t max_pages_per_seq;  /* 1 .. 2^26 */
     int32_t max_ctx_len;        /* upper bound on ctx_lens; sizes the worker count only */
-    int32_t num_workers;        /* 0: chosen by the library; the result does not depend on it
-                                   beyond rounding */
+    int32_t num_workers;        /* 0: chosen by the library; up to 2^16, fewer for shapes near the
+                                   limits above (the error names how many); the result does not
+                                   depend on it beyond rounding */
     int64_t num_pages;
 } ts_chunk_shape;
 

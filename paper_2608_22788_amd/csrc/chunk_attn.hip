@@ -863,7 +863,12 @@ int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
     // KV tiles of the call, from above
     const int64_t tiles = ((int64_t)s->num_tokens / pl->TT + std::min(s->num_seqs, s->num_tokens)) * s->num_kv_heads *
                           (((int64_t)s->max_ctx_len + kKeyTile - 1) / kKeyTile);
-    pl->W = s->num_workers > 0 ? s->num_workers : (int)std::max<int64_t>(1, std::min<int64_t>(256, tiles / 2));
+    const int64_t most = workers_bound(places_bound(s->num_seqs, s->num_kv_heads, s->num_tokens, pl->TT,
+                                                    (int64_t)s->max_pages_per_seq * kPage));
+    if (s->num_workers > most)
+        return fail(TS_ERR_SHAPE, "num_workers %d exceeds %lld, what this shape's work can be cut into", s->num_workers,
+                    (long long)most);
+    pl->W = s->num_workers > 0 ? s->num_workers : (int)std::max<int64_t>(1, std::min({(int64_t)256, tiles / 2, most}));
     const size_t rows = 2 * (size_t)pl->W * kTileRows;
     pl->ws_lse_off = rows * s->head_dim * sizeof(float);
     pl->ws_cut_off = pl->ws_lse_off + rows * sizeof(float);

@@ -78,6 +78,16 @@ struct ChunkSeq {
     TS_HOST_DEVICE int64_t total() const { return before(tiles()); }
 };
 
+// Places of a call from above, whatever its arrays hold (starts out of order can
+// give every sequence all the rows); below 2^62 for every accepted shape.  The
+// cut into W ranges multiplies places by W in 64 bits.
+inline int64_t places_bound(int seqs, int kv_heads, int rows, int TT, int64_t max_len) {
+    const int64_t tiles = ((int64_t)rows + TT - 1) / TT;
+    const int64_t keys = max_len > rows ? max_len : rows;
+    return (int64_t)seqs * kv_heads * tiles * (kTilePlaces * ((keys + kKeyTile - 1) / kKeyTile) + kUnitPlaces);
+}
+inline int64_t workers_bound(int64_t places) { return INT64_MAX / (places > 0 ? places : 1); }
+
 // First KV tile at or behind place `off` of a row tile.
 TS_HOST_DEVICE int tile_at(int64_t off, int weight) { return (int)((off + weight - 1) / weight); }
 
