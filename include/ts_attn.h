@@ -417,8 +417,9 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  * logarithm of the probability that the drawn token had among the kept ones (0
  * for the largest logit).  Logits of -inf and NaN have no mass, +inf reads as
  * the largest float32; a row without mass gives token -1 and logprob -inf.
- * Masses are integers in units of 2^-42 of the largest weight or finer, so
- * results do not depend on the order of sums.
+ * Masses are integers in units of at most 2^-41.5 of the largest weight, so
+ * results do not depend on the order of sums; a weight is off by at most 1.5
+ * units and by 2^-53 |l_v / temperature| of itself.
  *   logits       float32 or bf16 [num_seqs][vocab], rows row_stride elements
  *                apart (at least vocab, any alignment of an element);
  *                num_seqs 1 .. 65536, vocab 1 .. 2^20

@@ -13,13 +13,16 @@
 // the total: float32 sums would move the draw of about one row in ten.
 //
 // Masses.  x = l log2(e) / T in float64, n = rint(x), and 2^(x - n) by its
-// Taylor polynomial of degree 10 (|x - n| <= 1/2: off by less than 2^-42)
-// give a weight's 43-bit significand; relative to a power of two 2^E it is
-// that integer shifted right by E - n.  So masses are 64-bit integers in units
-// of 2^(E - 42): their sums do not depend on order, thread blocks of different
-// E join by a shift, and where the running sum passes a target is found block
-// by block, run by run and element by element with the same integers.  A
-// weight is off by at most a unit, 2^-42 of the largest.
+// Taylor polynomial of degree 10 give a weight's 43-bit significand; relative to
+// a power of two 2^E it is that integer shifted right by E - n.  So masses are
+// 64-bit integers in units of 2^(E - 42), at most 2^-41.5 of the largest weight:
+// their sums do not depend on order, thread blocks of different E join by a
+// shift, and where the running sum passes a target is found block by block, run
+// by run and element by element with the same integers.  The significand is off
+// by at most 1.48 (the series' end 0.98 at |x - n| = 1/2, its rounding 0.5), so a
+// weight by 1.5 units, the shift included.  x is rounded at its own size, not at
+// its distance from the maximum: by 2^-53 |l / T| of the weight, which passes a
+// unit for the largest ones where |l / T| passes about 2,000.
 //
 // What bounds it: the row is read once from memory, and a weight costs 22
 // float64-rate instructions (as many as float32 ones issue here), about as
