@@ -256,9 +256,9 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 // Loads kLoads blocks of 1 KiB into LDS without passing registers: block i from
 // byte (from ^ (twist i)) + 1024 i of the resource (each lane 16 bytes), to `to`
 // + 1024 i + 16 lane.  The instructions have no outputs, so nothing can be taken
-// for written before it is; m0, which they need, has no other use in these
-// kernels.  Completion is counted by vmcnt: dma_wait() and a barrier come before
-// the data is read.
+// for written before it is; m0, which they need, is named as overwritten.
+// Completion is counted by vmcnt: dma_wait() and a barrier come before the data
+// is read.
 //
 // Keys that one row tile alone reads (kOnce) are loaded as not to be kept: 256
 // sequences of one token behind 1,000 take 181 us so, 198 otherwise; a prompt,
@@ -272,16 +272,20 @@ __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int f
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept) TS_DMA_BLOCK("3", "1024", kept)    \
                          TS_DMA_BLOCK("4", "2048", kept) TS_DMA_BLOCK("5", "%6", kept)::"s"(to), "s"(rsrc), "v"(from), \
                      "v"(from ^ twist), "v"(from ^ 2 * twist), "v"(from ^ 3 * twist), "n"(3 * 1024)                    \
-                     : "memory");                                                                                      \
+                     : "m0", "memory");                                                                                \
     else                                                                                                               \
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept)                                   \
                          TS_DMA_BLOCK("3", "1024", kept)::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist)             \
-                     : "memory")
+                     : "m0", "memory")
+    // (a clobber of m0 warns that its value is not kept: nobody needs it)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
     if constexpr (kOnce) {
         TS_DMA_BLOCKS(" nt");
     } else {
         TS_DMA_BLOCKS("");
     }
+#pragma clang diagnostic pop
 #undef TS_DMA_BLOCKS
 #undef TS_DMA_BLOCK
 }
