@@ -230,6 +230,14 @@ def _own_workspace(nbytes: int, device, stream, zeros: bool = False):
         return (torch.zeros if zeros else torch.empty)(nbytes, dtype=torch.uint8, device=device)
 
 
+def _nbytes(workspace) -> int:
+    """Bytes that a workspace tensor spans (one that repeats its memory spans fewer
+    than it has elements)."""
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def shape_of(q, k_pages, page_table, max_ctx_len=None, num_workers=0, variant=0) -> AttnShape:
     B, Qmax, Hq, D = q.shape
     NP, Hkv, P, D2 = k_pages.shape
@@ -272,13 +280,12 @@ def decode_attn(q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale: f
     need = workspace_size(shape)
     if workspace is None:
         workspace = _own_workspace(need, q.device, stream, zeros=True)
-    elif workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes, "
-                         f"this call needs {need}")
+    have = _nbytes(workspace)
+    if have < need:
+        raise ValueError(f"workspace has {have} bytes, this call needs {need}")
     args = (ctypes.byref(shape), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
             page_table.data_ptr(), ctx_lens.data_ptr(), q_lens.data_ptr(), out.data_ptr(),
-            ctypes.c_float(scale), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+            ctypes.c_float(scale), workspace.data_ptr(), have, _stream_ptr(stream))
     if events is None:
         check(lib.ts_decode_attn(*args), "ts_decode_attn")
     else:
@@ -480,9 +487,7 @@ def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, 
     ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
     check(lib.ts_spec_accept(B, V, G, p_target.data_ptr(), ptr(q_draft), ptr(draft_tokens),
                              num_draft.data_ptr(), ptr(u_accept), u_sample.data_ptr(), num_accepted.data_ptr(),
-                             next_token.data_ptr(), workspace.data_ptr(),
-                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-          "ts_spec_accept")
+                             next_token.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream)), "ts_spec_accept")
     return workspace
 
 
@@ -598,8 +603,7 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
         workspace = _own_workspace(chunk_workspace_size(shape), q.device, stream)
     check(lib.ts_chunk_attn(ctypes.byref(shape), q.data_ptr(), q_stride, k_pages.data_ptr(), v_pages.data_ptr(),
                             page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
-                            out_stride, scale, workspace.data_ptr(),
-                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_chunk_attn")
+                            out_stride, scale, workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream)), "ts_chunk_attn")
     return workspace
 
 
@@ -631,6 +635,6 @@ def sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=N
         workspace = _own_workspace(sample_workspace_size(B, V), logits.device, stream)
     check(lib.ts_sample(B, V, LOGITS_F32 if logits.dtype == torch.float32 else LOGITS_BF16, logits.data_ptr(),
                         logits.stride(0) if B > 1 else V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-                        u.data_ptr(), token.data_ptr(), _ptr(logprob), workspace.data_ptr(),
-                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "ts_sample")
+                        u.data_ptr(), token.data_ptr(), _ptr(logprob), workspace.data_ptr(), _nbytes(workspace),
+                        _stream_ptr(stream)), "ts_sample")
     return workspace

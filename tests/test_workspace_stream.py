@@ -106,3 +106,12 @@ def test_workspace_is_made_on_the_calls_stream(recorded, call, kind):
     own = torch.ones(4096, dtype=torch.uint8)
     del made[:]
     assert call(side, workspace=own) is own and not made
+
+
+@pytest.mark.parametrize("call", [decode, accept, chunk, draw], ids=["decode_attn", "spec_accept", "chunk_attn", "sample"])
+def test_workspace_that_repeats_its_memory_is_refused(recorded, call):
+    """It has as many elements as the call needs bytes, and a single byte."""
+    _, launched = recorded
+    with pytest.raises(ValueError):
+        call(None, workspace=torch.ones(1, dtype=torch.uint8).expand(1 << 20))
+    assert not launched
