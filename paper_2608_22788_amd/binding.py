@@ -528,12 +528,14 @@ def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts):
     return (*pool, *table)
 
 
-def _check_device(*tensors) -> None:
-    """Every tensor lives on the current device, whose stream the call uses."""
+def _check_device(*tensors, stream=None) -> None:
+    """Every tensor lives on the current device, and so does the call's stream."""
     dev = torch.cuda.current_device() if tensors[0].is_cuda else None
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"every tensor must be on the current CUDA device ({dev}), one is on {t.device}")
+    if stream is not None and getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"the stream must be on the current CUDA device ({dev}), it is on {stream.device_index}")
 
 
 def _ptr(t):
@@ -578,7 +580,8 @@ def rope_append(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts
     for n, w in (("q_norm", q_norm), ("k_norm", k_norm)):
         if w is not None and (w.dtype != torch.bfloat16 or w.shape != (D,) or not w.is_contiguous()):
             raise ValueError(f"{n} must be a contiguous bf16 vector of head_dim values")
-    _check_device(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm)
+    _check_device(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm,
+                  stream=stream)
     shape = ChunkShape(B, T, Hq, Hkv, D, P, T, maxp, maxp * P, 0, NP)
     cfg = RopeConfig(rot, int(interleaved), eps, 0, q_stride, k_stride, v_stride, out_stride)
     check(lib.ts_rope_append(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -596,7 +599,7 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
     NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts)
     if not (T == To and Hq == Ho and D == Do == Dp):
         raise ValueError("out must match q, and head_dim that of the pages")
-    _check_device(q, out, k_pages, v_pages, page_table, ctx_lens, q_starts, workspace)
+    _check_device(q, out, k_pages, v_pages, page_table, ctx_lens, q_starts, workspace, stream=stream)
     shape = ChunkShape(B, T, Hq, Hkv, D, P, T if max_q_len is None else int(max_q_len), maxp,
                        maxp * P if max_ctx_len is None else int(max_ctx_len), num_workers, NP)
     if workspace is None:
@@ -630,7 +633,7 @@ def sample(logits, u, token, logprob=None, temperature=None, top_k=None, top_p=N
                         ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
         if t is not None and (t.dtype != dt or t.shape != rows or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous {dt} vector with a value per row")
-    _check_device(logits, u, token, logprob, temperature, top_k, top_p, min_p, workspace)
+    _check_device(logits, u, token, logprob, temperature, top_k, top_p, min_p, workspace, stream=stream)
     if workspace is None:
         workspace = _own_workspace(sample_workspace_size(B, V), logits.device, stream)
     check(lib.ts_sample(B, V, LOGITS_F32 if logits.dtype == torch.float32 else LOGITS_BF16, logits.data_ptr(),

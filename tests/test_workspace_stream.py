@@ -57,7 +57,7 @@ def recorded(monkeypatch):
     for kind in ("empty", "zeros"):
         monkeypatch.setattr(torch, kind, recording(kind))
     monkeypatch.setattr(binding, "lib", lib)
-    monkeypatch.setattr(binding, "_check_device", lambda *t: None)
+    monkeypatch.setattr(binding, "_check_device", lambda *t, **kw: None)
     monkeypatch.setattr(binding, "_check_tensors", lambda *t: None)
     monkeypatch.setattr(binding, "_stream_ptr", lambda s: 0 if s is None else s.cuda_stream)
     return made, lib.launched
