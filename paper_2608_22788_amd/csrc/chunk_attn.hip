@@ -8,7 +8,11 @@
 // m + 8, m moves up to it and what is summed so far is scaled by 2^(old - new).
 // Weights stay at 2^8 or below; they are rounded to bf16 for the second matrix
 // product, which takes no more, and their float32 sum takes the rounded ones too,
-// so that the result stays an average of values (two to an instruction).
+// so that the result stays an average of values (two to an instruction).  That
+// rounding is a choice: outputs are off by 2.1-2.3e-3 (rel-L2 against 64 bits),
+// of which the rounding of the result alone is 1.6-1.7e-3; a second product with
+// what it takes away brings that back and takes a prompt from 524 to 708 us, four
+// resumed rollouts from 436 to 575, a mixed batch from 77 to 86.
 //
 // Work.  A row tile is 256 rows of one KV head (256 / G tokens with their G query
 // heads each, so that a key is read once for the group), a KV tile 64 keys.  A
@@ -26,11 +30,12 @@
 // rows are stored in an order without bank conflicts (measured: none).
 //
 // What bounds it.  Long chunks: 4 D operations per row and key.  At 8,192 tokens
-// of a prompt, 32/8 heads, head_dim 128: 521 us, 1,055 TFLOP/s, 77 % of what a
-// 16384^3 bf16 product reaches on the card (533 us on another box).  The clock
-// falls to 2.0-2.2 GHz; of a SIMD's cycles the matrix unit is busy 54 %, and
-// other vector instructions (an exponential, a multiply-add and half a maximum, a
-// packing and a sum for each score) issue in 36 %.  What mattered, on that case:
+// of a prompt, 32/8 heads, head_dim 128: 521-557 us by box, 990-1,055 TFLOP/s,
+// 72-77 % of what a 16384^3 bf16 product reaches on the card.  The clock is about
+// 2 GHz; of a SIMD's cycles the matrix unit is busy 53 %, and other vector
+// instructions (an exponential, which takes two issue slots, a multiply-add and
+// half a maximum, a packing and a sum for each score) issue in 39 % (how far the
+// two overlap the counters do not say).  What mattered, on that case:
 //   - 128 rows on 4 wavefronts took 781 us: every CU then draws 10 TB/s of tiles
 //     through the L2s, which alone take 423 us; 256 rows halve that;
 //   - a tile's weights beside the next tile's scores, in a fixed order: 551 us
@@ -39,10 +44,12 @@
 //   - no effect: more of the weights beside the scores, wave priorities, operands
 //     read six products ahead instead of four; worse: two wavefronts to the halves
 //     of one tile (564 instead of 555), 64 rows per wavefront (726 instead of 522).
-// head_dim 64 has twice the exponentials per operation: 92 us for 56.9 GFLOP.
+// head_dim 64 has twice the exponentials per operation: 92-95 us for 56.9 GFLOP;
+// matrix unit 31 %, other vector instructions 47 % of a busy CU's cycles, and CUs
+// have work for 82 % of the kernel's time only (starts, ends).
 // Long caches under few rows: the cache's bytes, 16 KiB of K and as much of V per
 // tile.  32 sequences, most of them decoding behind up to 4,000 tokens: 77 us for
-// 317 MB; 256 sequences of one token behind 1,000: 183 us for 1,057 MB, 5.8 TB/s.
+// 317 MB; 256 sequences of one token behind 1,000: 181 us for 1,057 MB, 5.8 TB/s.
 // One short chunk (37 tokens behind 2,011, 23 us): the chain of a launch, finding
 // the work, two tiles and the join of 16 pieces.
 #include <hip/hip_runtime.h>
@@ -114,7 +121,7 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
 // Places of one head up to the end of each sequence, in s_end[0 .. B - 1]: a
 // thread per sequence, sums within wavefronts and then, past 64 sequences, over
 // them.  (With one wavefront for all of them a call of 4,096 sequences of 100
-// tokens took 924 us, so 811; one of 256 x 1,000 tokens 207, so 204.)
+// tokens took 113 us more; it takes 720.)
 __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
     const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     uint64_t base = 0;
