@@ -402,6 +402,38 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
                   const int32_t *q_starts, void *out, int64_t out_stride, float scale, void *workspace,
                   size_t workspace_bytes, void *stream);
 
+/* ---- the cache held in 8 bits ---------------------------------------------------
+ * The same pages with one byte a value, half of the bytes that attention reads:
+ *   k_pages, v_pages  e4m3 codes [num_pages][num_kv_heads][16][head_dim], 16-byte
+ *                     aligned
+ *   kv_scales         uint8 [num_pages][num_kv_heads][2], 16-byte aligned: the
+ *                     biased exponents (e8m0) of a power of two for the keys and
+ *                     one for the values of each page and KV head
+ * A cached value is code * 2^(byte - 127), exactly a bf16 number for the bytes 27
+ * to 227 that ts_rope_append_kv8 writes (the powers 2^-100 to 2^100); with others
+ * the product is taken as bf16 takes it.  Code 0x7f (and 0xff) is NaN; e4m3 has no
+ * infinity. */
+
+/* ts_rope_append into the cache held in 8 bits.  Norm and rotation in float32 as
+ * there, then for each page and KV head that receives tokens, for its keys and
+ * for its values x (float32, not rounded in between):
+ *   m = max |x| over the new tokens, 2^k the smallest power with m <= 448 * 2^k
+ *   (2^-100 if m is 0);
+ *   if the page holds tokens of this sequence in front of the new ones, with power
+ *   2^h, k becomes max(k, h) and their codes c become e4m3(c * 2^(h - k)): the
+ *   same value, but where it falls below 2^(k - 6) (e4m3's denormal range);
+ *   code = e4m3(x / 2^k), nearest even.
+ * Powers stay inside 2^-100 .. 2^100 and larger values are held as +-448 * 2^100.
+ * Infinite and NaN values are held as NaN and do not count for m.  The bytes that
+ * a page held behind its last token are not looked at, and kept.  Two sequences
+ * must not append to one page in one call, as they must not to one slot of the
+ * bf16 cache.  Otherwise arguments, limits and errors are those of
+ * ts_rope_append. */
+int ts_rope_append_kv8(const ts_chunk_shape *shape, const ts_rope_config *cfg, const void *q, const void *k,
+                       const void *v, void *q_out, void *k_pages, void *v_pages, void *kv_scales,
+                       const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts,
+                       const float *inv_freq, const void *q_norm, const void *k_norm, void *stream);
+
 /* ---- sampling ------------------------------------------------------------------
  * Draws each sequence's next token from its row of logits l, with the rule of
  * ts_spec_accept (the smallest token whose cumulative mass exceeds u times the

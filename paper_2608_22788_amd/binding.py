@@ -88,7 +88,8 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_version", "ts_tau_table", "ts_replica_time", "ts_request_shares", "ts_step_makespan",
            "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
            "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn",
-           "ts_sample_workspace_size", "ts_sample"]
+           "ts_sample_workspace_size", "ts_sample",
+           "ts_rope_append_kv8"]
 
 
 def _load() -> ctypes.CDLL:
@@ -165,6 +166,8 @@ def _load() -> ctypes.CDLL:
     lib.ts_sample_workspace_size.restype = SZ
     lib.ts_sample.argtypes = [I32, I32, I32, P, I64, P, P, P, P, P, P, P, P, SZ, P]
     lib.ts_sample.restype = ctypes.c_int
+    lib.ts_rope_append_kv8.argtypes = [pchunk, ctypes.POINTER(RopeConfig)] + [P] * 14
+    lib.ts_rope_append_kv8.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
     lib.ts_status_string.restype = ctypes.c_char_p
     lib.ts_last_error.argtypes = []
@@ -512,11 +515,11 @@ def _rows(t, name: str):
     raise ValueError(f"{name} must be a bf16 tensor [tokens][heads][head_dim] whose heads are contiguous")
 
 
-def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts):
+def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts, dtype=_BF16):
     """(num_pages, kv_heads, page size, head_dim, sequences, pages per sequence)."""
-    if not (k_pages.dtype is _BF16 and v_pages.dtype is _BF16 and page_table.dtype is _I32 and ctx_lens.dtype is _I32 and
+    if not (k_pages.dtype is dtype and v_pages.dtype is dtype and page_table.dtype is _I32 and ctx_lens.dtype is _I32 and
             q_starts.dtype is _I32):
-        raise ValueError("k_pages and v_pages must be bf16, page_table, ctx_lens and q_starts int32 tensors")
+        raise ValueError(f"k_pages and v_pages must be {dtype}, page_table, ctx_lens and q_starts int32 tensors")
     if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous() and
             ctx_lens.is_contiguous() and q_starts.is_contiguous()):
         raise ValueError("k_pages, v_pages, page_table, ctx_lens and q_starts must be contiguous")
@@ -565,11 +568,22 @@ def rope_append(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts
     """ts_rope_append on torch tensors: q, q_out bf16 [T][Hq][D], k, v bf16
     [T][Hkv][D] (rows may be strided, as views of one projection's output are),
     inv_freq float32 [rot_dim / 2] or None, norms bf16 [D] or None."""
+    shape, cfg = _rope_args(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm,
+                            eps, interleaved, stream, _BF16)
+    check(lib.ts_rope_append(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                             q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                             ctx_lens.data_ptr(), q_starts.data_ptr(), _ptr(inv_freq), _ptr(q_norm), _ptr(k_norm),
+                             _stream_ptr(stream)), "ts_rope_append")
+
+
+def _rope_args(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm, eps,
+               interleaved, stream, dtype, *others):
+    """The shape and configuration of an append, its tensors checked."""
     T, Hq, D, q_stride = _rows(q, "q")
     Tk, Hk, Dk, k_stride = _rows(k, "k")
     Tv, Hv, Dv, v_stride = _rows(v, "v")
     To, Ho, Do, out_stride = _rows(q_out, "q_out")
-    NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts)
+    NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts, dtype)
     if not (T == Tk == Tv == To and Hq == Ho and Hkv == Hk == Hv and D == Dk == Dv == Do == Dp):
         raise ValueError("q_out must match q, and k and v must be [tokens][kv_heads][head_dim]")
     rot = 0
@@ -581,13 +595,9 @@ def rope_append(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts
         if w is not None and (w.dtype != torch.bfloat16 or w.shape != (D,) or not w.is_contiguous()):
             raise ValueError(f"{n} must be a contiguous bf16 vector of head_dim values")
     _check_device(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm,
-                  stream=stream)
-    shape = ChunkShape(B, T, Hq, Hkv, D, P, T, maxp, maxp * P, 0, NP)
-    cfg = RopeConfig(rot, int(interleaved), eps, 0, q_stride, k_stride, v_stride, out_stride)
-    check(lib.ts_rope_append(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                             q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                             ctx_lens.data_ptr(), q_starts.data_ptr(), _ptr(inv_freq), _ptr(q_norm), _ptr(k_norm),
-                             _stream_ptr(stream)), "ts_rope_append")
+                  *others, stream=stream)
+    return (ChunkShape(B, T, Hq, Hkv, D, P, T, maxp, maxp * P, 0, NP),
+            RopeConfig(rot, int(interleaved), eps, 0, q_stride, k_stride, v_stride, out_stride))
 
 
 def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: float, workspace=None,
@@ -608,6 +618,29 @@ def chunk_attn(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, scale: 
                             page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), out.data_ptr(),
                             out_stride, scale, workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream)), "ts_chunk_attn")
     return workspace
+
+
+# ---- the cache held in 8 bits ---------------------------------------------------
+
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def _check_scales(kv_scales, k_pages) -> None:
+    if kv_scales.dtype is not _E8M0 or kv_scales.shape != (*k_pages.shape[:2], 2) or not kv_scales.is_contiguous():
+        raise ValueError(f"kv_scales must be a contiguous {_E8M0} tensor [num_pages][kv_heads][2]")
+
+
+def rope_append_kv8(q, k, v, q_out, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_starts, inv_freq, q_norm=None,
+                    k_norm=None, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """ts_rope_append_kv8 on torch tensors: as rope_append, with pages float8_e4m3fn
+    [num_pages][Hkv][16][D] and kv_scales float8_e8m0fnu [num_pages][Hkv][2]."""
+    _check_scales(kv_scales, k_pages)
+    shape, cfg = _rope_args(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm,
+                            eps, interleaved, stream, _E4M3, kv_scales)
+    check(lib.ts_rope_append_kv8(ctypes.byref(shape), ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                 q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), kv_scales.data_ptr(),
+                                 page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), _ptr(inv_freq),
+                                 _ptr(q_norm), _ptr(k_norm), _stream_ptr(stream)), "ts_rope_append_kv8")
 
 
 # ---- sampling ------------------------------------------------------------------

@@ -30,6 +30,7 @@
 
 #include "attn_common.h"
 #include "chunk_common.h"
+#include "rope_common.h"
 #include "ts_attn.h"
 #include "ts_internal.h"
 
@@ -58,30 +59,6 @@ struct RowInfo {
     int64_t slot;             // (page * Hkv * 16 + position % 16), or -1: no place in the pool
     int used;                 // the row belongs to a sequence
 };
-
-__device__ __forceinline__ void unpack8(u32x4_t u, float x[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        x[2 * i] = bf16_lo(u[i]);
-        x[2 * i + 1] = bf16_hi(u[i]);
-    }
-}
-__device__ __forceinline__ u32x4_t pack8(const float x[8]) {
-    u32x4_t u;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        u[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    return u;
-}
-
-constexpr int kDppMirror = 0x140;   // lane i <-> 15 - i within 16
-template <int kLanes>
-__device__ __forceinline__ float sum_head(float x) {
-    x = sum8(x);
-    if constexpr (kLanes == 16)
-        x += dpp_f32<kDppMirror>(x);
-    return x;
-}
 
 template <int D>
 __global__ __launch_bounds__(kRopeWaves * kWave) void rope_append_kernel(RopeParams p) {
@@ -207,17 +184,9 @@ __global__ __launch_bounds__(kRopeWaves * kWave) void rope_append_kernel(RopePar
 
 }  // namespace
 
-}  // namespace tsattn
-
-using namespace tsattn;
-
-extern "C" {
-
-int ts_rope_append(const ts_chunk_shape *s, const ts_rope_config *cfg, const void *q, const void *k, const void *v,
-                   void *q_out, void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens,
-                   const int32_t *q_starts, const float *inv_freq, const void *q_norm, const void *k_norm,
-                   void *stream) {
-    clear_error();
+int check_rope(const ts_chunk_shape *s, const ts_rope_config *cfg, const void *q, const void *k, const void *v,
+               void *q_out, void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens,
+               const int32_t *q_starts, const float *inv_freq, const void *q_norm, const void *k_norm) {
     int st = check_chunk_shape(s);
     if (st)
         return st;
@@ -246,8 +215,27 @@ int ts_rope_append(const ts_chunk_shape *s, const ts_rope_config *cfg, const voi
         return st;
     if (q_out == q && cfg->q_out_stride != cfg->q_stride)
         return fail(TS_ERR_ARG, "q_out == q needs equal strides");
+    return TS_OK;
+}
+
+}  // namespace tsattn
+
+using namespace tsattn;
+
+extern "C" {
+
+int ts_rope_append(const ts_chunk_shape *s, const ts_rope_config *cfg, const void *q, const void *k, const void *v,
+                   void *q_out, void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *ctx_lens,
+                   const int32_t *q_starts, const float *inv_freq, const void *q_norm, const void *k_norm,
+                   void *stream) {
+    clear_error();
+    int st = check_rope(s, cfg, q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm,
+                        k_norm);
+    if (st || s->num_tokens == 0)
+        return st;
     if ((st = check_device()))
         return st;
+    const int D = s->head_dim;
     RopeParams p;
     p.q = static_cast<const uint16_t *>(q);
     p.k = static_cast<const uint16_t *>(k);

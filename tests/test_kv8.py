@@ -1,0 +1,69 @@
+"""The operators over the cache held in 8 bits without a GPU: their refusals
+before any HIP call, and the oracle's e4m3 against torch's."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8
+from paper_2608_22788_amd import binding as b
+from test_chunk import BAD_SHAPES, config, shape
+
+
+def append(s, cfg, q=16, k=16, v=16, out=16, kp=16, vp=16, scales=16, table=16, ctx=16, starts=16, freq=16, qn=None,
+           kn=None):
+    return b.lib.ts_rope_append_kv8(ctypes.byref(s) if s else None, ctypes.byref(cfg) if cfg else None, q, k, v, out,
+                                    kp, vp, scales, table, ctx, starts, freq, qn, kn, None)
+
+
+@pytest.mark.parametrize("kw", BAD_SHAPES, ids=str)
+def test_append_bad_shapes_rejected(kw):
+    assert append(shape(**kw), config()) == -2
+
+
+def test_append_arguments_rejected():
+    s, c = shape(), config()
+    assert append(None, c) == -1 and append(s, None) == -1
+    for name in ("q", "k", "v", "out", "kp", "vp", "scales", "table", "ctx", "starts", "freq"):
+        assert append(s, c, **{name: None}) == -1, name
+    for name in ("q", "k", "v", "out", "kp", "vp", "scales", "qn", "kn"):
+        assert append(s, c, **{name: 24}) == -6, name
+    for kw in (dict(rot_dim=24), dict(rot_dim=80), dict(rot_dim=-16), dict(interleaved=2), dict(reserved=1),
+               dict(q_stride=504), dict(k_stride=120), dict(v_stride=132), dict(q_out_stride=0)):
+        assert append(s, config(**kw)) == -6, kw
+    assert append(s, config(eps=float("nan")), qn=16) == -6
+    assert append(shape(num_tokens=0, max_q_len=0), None, q=None, scales=None) == 0
+
+
+def test_binding_refuses_other_types():
+    bf, e4, e8 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    rows = lambda h: torch.zeros(3, h, 64, dtype=bf)  # noqa: E731
+    args = dict(q=rows(4), k=rows(2), v=rows(2), q_out=rows(4), k_pages=torch.zeros(5, 2, 16, 64).to(e4),
+                v_pages=torch.zeros(5, 2, 16, 64).to(e4), kv_scales=torch.zeros(5, 2, 2, dtype=torch.uint8).view(e8),
+                page_table=i32(1, 2), ctx_lens=i32(1), q_starts=i32(2), inv_freq=None)
+    for name, bad in (("k_pages", torch.zeros(5, 2, 16, 64, dtype=bf)), ("v_pages", torch.zeros(5, 2, 16, 64, dtype=bf)),
+                      ("kv_scales", torch.zeros(5, 2, 2, dtype=torch.uint8)), ("kv_scales", args["kv_scales"][:4]),
+                      ("kv_scales", args["kv_scales"][..., :1])):
+        with pytest.raises(ValueError, match=name):
+            b.rope_append_kv8(**{**args, name: bad})
+    with pytest.raises(ValueError, match="CUDA"):
+        b.rope_append_kv8(**args)
+
+
+def test_oracle_codes_are_e4m3():
+    codes = torch.arange(256, dtype=torch.uint8)
+    mine, theirs = kv8.code_values(), codes.view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(mine, theirs, equal_nan=True)
+    x = np.abs(mine[np.isfinite(mine)])
+    grid = np.unique(x)
+    for lo, hi in zip(grid[:-1], grid[1:]):
+        assert hi - lo <= 2 * kv8.half_step(hi) and (hi - lo) / 2 == kv8.half_step(lo)
+
+
+@pytest.mark.parametrize("amax,byte", [(448.0, 127), (448.0001, 128), (224.0, 126), (1.75, 119), (1.7500001, 120),
+                                       (0.0, 27), (1e-30, 27), (3e38, 227), (2.0 ** -92, 27), (1.75 * 2.0 ** -91, 28)])
+def test_oracle_power(amax, byte):
+    assert kv8.power_byte(amax) == byte
+    assert amax <= 448.0 * 2.0 ** (byte - 127) or byte == 227
