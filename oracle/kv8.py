@@ -76,7 +76,7 @@ def append(q, k, v, k_codes, v_codes, scales, table, ctx, starts, inv_freq, q_no
                         byte = min(max(byte, int(scales[pid, g, which])), HIGHEST)
                         held = number[codes[pid, g, :lo]] * 2.0 ** (int(scales[pid, g, which]) - byte)
                         want[which][pid, g, :lo] = np.where(np.isnan(held), np.inf, held)
-                XX
-                    want[which][pid, g, lo:hi] = np.where(np.isfinite(new), new, np.inf)
+                    scaled = np.clip(new / 2.0 ** (byte - 127), -448.0, 448.0)
+                    want[which][pid, g, lo:hi] = np.where(np.isfinite(new), scaled, np.inf)
                     scales[pid, g, which] = byte
     return q_out, want[0], want[1], scales
