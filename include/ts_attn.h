@@ -434,6 +434,60 @@ int ts_rope_append_kv8(const ts_chunk_shape *shape, const ts_rope_config *cfg, c
                        const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts,
                        const float *inv_freq, const void *q_norm, const void *k_norm, void *stream);
 
+/* ---- rules on logits -------------------------------------------------------------
+ * What a request asks of its row of logits before ts_sample draws from it:
+ * penalties for tokens that its text holds, biases and a grammar's mask.  For
+ * token v of row b with logit l, in float32 and in this order:
+ *   x = l;
+ *   v among the row's tokens:  x = x > 0 ? x / repetition : x * repetition;
+ *   v n > 0 times among those behind the prompt:
+ *                              x = x - (frequency * n + presence);
+ *   biases of v in the row's list:  x = x + their sum, added up in list order;
+ *   v not allowed:             x = -inf;
+ *   out = x, rounded once.  Infinite and NaN logits go the same way.
+ * A row whose mask allows nothing is all -inf (ts_sample gives token -1 for it).
+ *   logits, out  float32 or bf16 [num_seqs][vocab], each with its type and its rows
+ *                row_stride / out_stride elements apart (at least vocab, any
+ *                alignment of an element); out may be logits itself, with one type
+ *                and stride, and must not overlap them otherwise; num_seqs 1 ..
+ *                65536, vocab 1 .. 2^20.  In place, only what the rules change is
+ *                read or written.
+ *   tokens       int32 [num_seqs][max_tokens], rows token_stride apart: each row's
+ *                text, prompt first; ids outside [0, vocab) count nowhere
+ *   lens, prompt_lens  int32 [num_seqs], clamped to [0, max_tokens] and [0, lens];
+ *                prompt_lens may be NULL (0)
+ *   repetition, frequency, presence  float32 [num_seqs]; each may be NULL, and a value
+ *                that is not finite (repetition: or not above 0) is off
+ *   bias_starts  int32 [num_seqs + 1], clamped to [0, num_biases]: row b has entries
+ *                bias_starts[b] .. bias_starts[b + 1] - 1 of
+ *   bias_tokens, bias_values  int32 and float32 [num_biases]; a token may appear more
+ *                than once, ids outside [0, vocab) count nowhere, any value is added
+ *                as it is (-inf bans a token)
+ *   allowed      uint32 [num_seqs][vocab / 32, rounded up], rows allowed_stride words
+ *                apart: token v is allowed if bit v % 32 of word v / 32 is set
+ * Without tokens, without all three bias arrays, without allowed (NULL) that rule is
+ * off.  Asynchronous on `stream`, one launch, no workspace; results do not depend
+ * on any order but the lists'. */
+#define TS_LOGITS_F32 0
+#define TS_LOGITS_BF16 1
+
+typedef struct ts_rules_config {
+    int32_t num_seqs;
+    int32_t vocab;
+    int32_t logits_type;        /* TS_LOGITS_F32 or TS_LOGITS_BF16 */
+    int32_t out_type;
+    int32_t max_tokens;         /* up to 2^30; used with tokens */
+    int32_t num_biases;         /* up to 2^30; used with biases */
+    int64_t row_stride, out_stride;   /* elements */
+    int64_t token_stride;       /* elements, at least max_tokens */
+    int64_t allowed_stride;     /* words, at least vocab / 32, rounded up */
+} ts_rules_config;
+
+int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, const int32_t *tokens,
+                   const int32_t *lens, const int32_t *prompt_lens, const float *repetition, const float *frequency,
+                   const float *presence, const int32_t *bias_starts, const int32_t *bias_tokens,
+                   const float *bias_values, const uint32_t *allowed, void *stream);
+
 /* ---- sampling ------------------------------------------------------------------
  * Draws each sequence's next token from its row of logits l, with the rule of
  * ts_spec_accept (the smallest token whose cumulative mass exceeds u times the
@@ -463,9 +517,6 @@ int ts_rope_append_kv8(const ts_chunk_shape *shape, const ts_rope_config *cfg, c
  * 256-byte aligned, any contents) carries the slices' sums and the candidates
  * between the call's launches, two without filters (all three NULL) and four
  * with them; calls that may run concurrently need distinct ones. */
-#define TS_LOGITS_F32 0
-#define TS_LOGITS_BF16 1
-
 size_t ts_sample_workspace_size(int32_t num_seqs, int32_t vocab);
 
 int ts_sample(int32_t num_seqs, int32_t vocab, int32_t logits_type, const void *logits,

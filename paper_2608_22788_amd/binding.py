@@ -61,6 +61,13 @@ class RopeConfig(ctypes.Structure):
                 ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64)]
 
 
+class RulesConfig(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logits_type", ctypes.c_int32),
+                ("out_type", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("num_biases", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("allowed_stride", ctypes.c_int64)]
+
+
 class SweepConfig(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("num_batches", ctypes.c_int32),
@@ -89,7 +96,7 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
            "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn",
            "ts_sample_workspace_size", "ts_sample",
-           "ts_rope_append_kv8"]
+           "ts_rope_append_kv8", "ts_logit_rules"]
 
 
 def _load() -> ctypes.CDLL:
@@ -168,6 +175,8 @@ def _load() -> ctypes.CDLL:
     lib.ts_sample.restype = ctypes.c_int
     lib.ts_rope_append_kv8.argtypes = [pchunk, ctypes.POINTER(RopeConfig)] + [P] * 14
     lib.ts_rope_append_kv8.restype = ctypes.c_int
+    lib.ts_logit_rules.argtypes = [ctypes.POINTER(RulesConfig)] + [P] * 13
+    lib.ts_logit_rules.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
     lib.ts_status_string.restype = ctypes.c_char_p
     lib.ts_last_error.argtypes = []
@@ -643,7 +652,58 @@ def rope_append_kv8(q, k, v, q_out, k_pages, v_pages, kv_scales, page_table, ctx
                                  _ptr(q_norm), _ptr(k_norm), _stream_ptr(stream)), "ts_rope_append_kv8")
 
 
-# ---- sampling ------------------------------------------------------------------
+# ---- rules on logits, sampling ---------------------------------------------------
+
+_LOGITS = {torch.float32: LOGITS_F32, torch.bfloat16: LOGITS_BF16}
+
+
+def logit_rules(logits, out, tokens=None, lens=None, prompt_lens=None, repetition=None, frequency=None, presence=None,
+                bias_starts=None, bias_tokens=None, bias_values=None, allowed=None, stream=None) -> None:
+    """ts_logit_rules on torch tensors: logits and out (or logits again) float32 or
+    bf16 [B][V], tokens int32 [B][N] (rows of all three may be strided), lens and
+    prompt_lens int32 [B], penalties float32 [B], bias_starts int32 [B + 1] with
+    bias_tokens int32 and bias_values float32 [M], allowed int32 [B][ceil(V / 32)]
+    (bits; rows may be strided); all but logits and out may be None."""
+    for name, t in (("logits", logits), ("out", out)):
+        if t.dtype not in _LOGITS or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must be a float32 or bf16 tensor [B][V] whose rows are contiguous")
+    B, V = logits.shape
+    if out.shape != logits.shape:
+        raise ValueError("out must have the shape of logits")
+    cfg = RulesConfig(B, V, _LOGITS[logits.dtype], _LOGITS[out.dtype], 0, 0, logits.stride(0) if B > 1 else V,
+                      out.stride(0) if B > 1 else V, 0, 0)
+    for name, t, dt, n in (("lens", lens, _I32, B), ("prompt_lens", prompt_lens, _I32, B),
+                           ("repetition", repetition, torch.float32, B), ("frequency", frequency, torch.float32, B),
+                           ("presence", presence, torch.float32, B), ("bias_starts", bias_starts, _I32, B + 1)):
+        if t is not None and (t.dtype is not dt or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dt} vector of {n} values")
+    if tokens is not None:
+        if tokens.dtype is not _I32 or tokens.dim() != 2 or tokens.shape[0] != B or (tokens.shape[1] > 1 and tokens.stride(1) != 1):
+            raise ValueError("tokens must be an int32 tensor [B][N] whose rows are contiguous")
+        cfg.max_tokens = N = tokens.shape[1]
+        cfg.token_stride = tokens.stride(0) if B > 1 and N > 0 else N
+    if bias_tokens is not None or bias_values is not None:
+        if (bias_tokens is None or bias_values is None or bias_tokens.dtype is not _I32 or
+                bias_values.dtype is not torch.float32 or bias_tokens.dim() != 1 or
+                bias_tokens.shape != bias_values.shape or
+                not (bias_tokens.is_contiguous() and bias_values.is_contiguous())):
+            raise ValueError("bias_tokens and bias_values must be contiguous int32 and float32 vectors of one length")
+        cfg.num_biases = bias_tokens.numel()
+    if allowed is not None:
+        words = (V + 31) // 32
+        if allowed.dtype is not _I32 or allowed.shape != (B, words) or (words > 1 and allowed.stride(1) != 1):
+            raise ValueError(f"allowed must be an int32 tensor [B][{words}] whose rows are contiguous")
+        cfg.allowed_stride = allowed.stride(0) if B > 1 else words
+    _check_device(logits, out, tokens, lens, prompt_lens, repetition, frequency, presence, bias_starts, bias_tokens,
+                  bias_values, allowed, stream=stream)
+    if cfg.num_biases == 0 and bias_tokens is not None:
+        bias_starts = bias_tokens = bias_values = None   # (an empty tensor has no address)
+    if tokens is not None and cfg.max_tokens == 0:
+        tokens = lens = prompt_lens = repetition = frequency = presence = None
+    check(lib.ts_logit_rules(ctypes.byref(cfg), logits.data_ptr(), out.data_ptr(), _ptr(tokens), _ptr(lens),
+                             _ptr(prompt_lens), _ptr(repetition), _ptr(frequency), _ptr(presence), _ptr(bias_starts),
+                             _ptr(bias_tokens), _ptr(bias_values), _ptr(allowed), _stream_ptr(stream)), "ts_logit_rules")
+
 
 def sample_workspace_size(num_seqs: int, vocab: int) -> int:
     n = lib.ts_sample_workspace_size(num_seqs, vocab)

@@ -1,0 +1,332 @@
+// logit_rules.hip -- what a request asks of its logits before the draw: penalties
+// for tokens that its text holds already, biases, and a grammar's mask.
+//
+// For token v of a row with logit l, with n the number of times that v is among
+// the row's answer (its tokens behind the prompt) and "seen" if it is among its
+// tokens at all, in float32 and in this order:
+//   x = l;  seen: x = x > 0 ? x / repetition : x * repetition;
+//   n > 0: x -= frequency * n + presence;  biased: x += the sum of v's biases;
+//   not allowed: x = -inf;  out = x, rounded once.
+//
+// A workgroup takes kSlice tokens of the vocabulary of one row, eight to a thread.
+// It counts the row's tokens that fall into its slice in LDS (integers, so the
+// order of the additions does not matter), reading all of the row's tokens: rows
+// have few thousands of them, and the slices of a row are neighbours on one XCD,
+// whose L2 holds them.  Its logits are on their way meanwhile.  Biases are added up
+// in LDS too, in the order of the list whatever threads they fall to: of the
+// threads that hold biases of one token, the first adds its own, then the next.
+// One launch, nothing kept in memory between slices or calls.
+//
+// In place, a thread that has nothing to change neither reads nor writes.
+//
+// What bounds it: memory where there are many rows (logits in and out, the mask,
+// the tokens); the chain lengths -> tokens -> LDS -> stores where there are few.
+#include <hip/hip_runtime.h>
+
+#include "attn_common.h"
+#include "ts_attn.h"
+#include "ts_internal.h"
+
+namespace tsattn {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kPer = 8;                        // tokens of a thread
+constexpr int kSlice = kThreads * kPer;
+constexpr int kAhead = 4;                      // groups of four text tokens whose loads are in flight together
+constexpr uint32_t kInPrompt = 0x80000000u;
+
+struct RulesParams {
+    const void *logits;
+    void *out;
+    const int32_t *tokens, *lens, *prompt_lens;
+    const float *repetition, *frequency, *presence;
+    const int32_t *bias_starts, *bias_tokens;
+    const float *bias_values;
+    const uint32_t *allowed;
+    int64_t row_stride, out_stride, token_stride, allowed_stride;
+    int vocab, slices, max_tokens, num_biases;
+    bool in_place;
+};
+
+// Loads and stores of any element alignment.
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Many {
+    T x[N];
+};
+
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ float value_of(uint16_t x) { return bf16_lo(x); }
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *src, int n, float x[kPer]) {
+    if (n >= kPer) {
+        const auto v = *reinterpret_cast<const Many<T, kPer> *>(src);
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+            x[e] = value_of(v.x[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+            x[e] = e < n ? value_of(src[e]) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store8(float *dst, int n, const float x[kPer]) {
+    if (n >= kPer) {
+        Many<float, kPer> v;
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+            v.x[e] = x[e];
+        *reinterpret_cast<Many<float, kPer> *>(dst) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+            if (e < n)
+                dst[e] = x[e];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t *dst, int n, const float x[kPer]) {
+    Many<uint32_t, kPer / 2> v;
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2)
+        v.x[e / 2] = pack_bf16x2(x[e], x[e + 1]);
+    if (n >= kPer) {
+        __builtin_memcpy(dst, &v, sizeof v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPer; e++)
+            if (e < n)
+                dst[e] = (uint16_t)(v.x[e / 2] >> 16 * (e % 2));
+    }
+}
+
+// A barrier for what is in LDS: loads from memory stay under way.
+__device__ __forceinline__ void lds_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A penalty, or `off` where it is not given or not finite.
+__device__ __forceinline__ float penalty(const float *p, int b, float off) {
+    const float x = p ? p[b] : off;
+    return fabsf(x) < INFINITY ? x : off;
+}
+
+template <typename TI, typename TO>
+__global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
+    extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+    uint32_t *const count = lds;                              // [kSlice] times in the answer; kInPrompt
+    float *const bias = reinterpret_cast<float *>(lds + kSlice);   // [kSlice], where there are biases
+    __shared__ int s_pending;
+    const int at = xcd_worker(blockIdx.x, gridDim.x);
+    const int b = at / p.slices, base = at % p.slices * kSlice, tid = threadIdx.x;
+    const int n = p.vocab - base - kPer * tid;                // of this thread's tokens exist
+    const TI *const src = static_cast<const TI *>(p.logits) + b * p.row_stride + base + kPer * tid;
+    TO *const dst = static_cast<TO *>(p.out) + b * p.out_stride + base + kPer * tid;
+    float x[kPer];
+    if (!p.in_place)
+        load8(src, n, x);
+    uint32_t closed = 0;                                      // bit e: token e is not allowed
+    if (p.allowed && n > 0) {
+        const int v = base + kPer * tid;
+        closed = ~p.allowed[b * p.allowed_stride + v / 32] >> v % 32 & 0xff;
+    }
+    u32x4_t *const zero = reinterpret_cast<u32x4_t *>(lds);
+#pragma unroll
+    for (int i = 0; i < kSlice / 4 / kThreads; i++) {
+        zero[i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
+        if (p.bias_tokens)
+            zero[kSlice / 4 + i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
+    }
+    lds_sync();
+
+    if (p.bias_tokens) {
+        const int first = min(max(ld_meta(p.bias_starts, b), 0), p.num_biases);
+        const int end = min(max(ld_meta(p.bias_starts, b + 1), 0), p.num_biases);
+        for (int j0 = first; j0 < end; j0 += kThreads) {
+            const int j = j0 + tid;
+            const uint32_t t = j < end ? (uint32_t)p.bias_tokens[j] - (uint32_t)base : ~0u;
+            bool pending = t < (uint32_t)min(kSlice, p.vocab - base);
+            const float w = pending ? p.bias_values[j] : 0.0f;
+            const uint32_t mine = kThreads - tid;             // the first thread has the largest
+            for (;;) {
+                if (tid == 0)
+                    s_pending = 0;
+                if (pending)
+                    atomicMax(&count[t], mine);
+                lds_sync();
+                const bool turn = pending && count[t] == mine;
+                if (pending && !turn)
+                    s_pending = 1;
+                lds_sync();
+                if (turn) {
+                    bias[t] += w;
+                    count[t] = 0;
+                    pending = false;
+                }
+                const int more = s_pending;
+                lds_sync();
+                if (!more)
+                    break;
+            }
+        }
+    }
+
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+    if (p.tokens) {
+        const int len = min(max(ld_meta(p.lens, b), 0), p.max_tokens);
+        const int prompt = p.prompt_lens ? min(max(ld_meta(p.prompt_lens, b), 0), len) : 0;
+        const int32_t *const text = p.tokens + b * p.token_stride;
+        const uint32_t here = (uint32_t)min(kSlice, p.vocab - base);
+        const auto add = [&](int i, int32_t token) {
+            const uint32_t t = (uint32_t)token - (uint32_t)base;
+            if (t < here) {
+                if (i < prompt)
+                    atomicOr(&count[t], kInPrompt);
+                else
+                    atomicAdd(&count[t], 1u);
+            }
+        };
+        const int whole = len / 4 * 4;
+        for (int i0 = 4 * tid; i0 < whole; i0 += 4 * kThreads * kAhead) {
+            Many<int32_t, 4> v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; k++)
+                v[k] = *reinterpret_cast<const Many<int32_t, 4> *>(text + (i0 + 4 * kThreads * k < whole ? i0 + 4 * kThreads * k : i0));
+#pragma unroll
+            for (int k = 0; k < kAhead; k++)
+                if (i0 + 4 * kThreads * k < whole)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        add(i0 + 4 * kThreads * k + e, v[k].x[e]);
+        }
+        if (whole + tid < len)
+            add(whole + tid, text[whole + tid]);
+        rep = penalty(p.repetition, b, 1.0f);
+        rep = rep > 0.0f ? rep : 1.0f;
+        freq = penalty(p.frequency, b, 0.0f);
+        pres = penalty(p.presence, b, 0.0f);
+        lds_sync();
+    }
+    if (n <= 0)
+        return;
+    uint32_t c[kPer];
+    float w[kPer];
+    uint32_t any = closed;
+#pragma unroll
+    for (int e = 0; e < kPer; e += 4) {
+        const u32x4_t cv = *reinterpret_cast<const u32x4_t *>(count + kPer * tid + e);
+        f32x4_t wv = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.bias_tokens)
+            wv = *reinterpret_cast<const f32x4_t *>(bias + kPer * tid + e);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            c[e + i] = cv[i];
+            w[e + i] = wv[i];
+            any |= cv[i] | (wv[i] != 0.0f);   // (NaN differs from 0)
+        }
+    }
+    if (p.in_place) {
+        if (!any)
+            return;
+        load8(src, n, x);
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; e++) {
+        if (c[e]) {
+            const uint32_t times = c[e] & ~kInPrompt;
+            x[e] = x[e] > 0.0f ? x[e] / rep : x[e] * rep;
+            x[e] -= times ? freq * (float)times + pres : 0.0f;
+        }
+        x[e] += w[e];
+        x[e] = closed >> e & 1 ? -INFINITY : x[e];
+    }
+    store8(dst, n, x);
+}
+
+}  // namespace
+
+}  // namespace tsattn
+
+using namespace tsattn;
+
+extern "C" {
+
+int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, const int32_t *tokens,
+                   const int32_t *lens, const int32_t *prompt_lens, const float *repetition, const float *frequency,
+                   const float *presence, const int32_t *bias_starts, const int32_t *bias_tokens,
+                   const float *bias_values, const uint32_t *allowed, void *stream) {
+    clear_error();
+    if (!cfg || !logits || !out)
+        return fail(TS_ERR_NULL, "a pointer is NULL");
+    if (cfg->num_seqs < 1 || cfg->num_seqs > 65536)
+        return fail(TS_ERR_SHAPE, "num_seqs %d outside [1, 65536]", cfg->num_seqs);
+    if (cfg->vocab < 1 || cfg->vocab > (1 << 20))
+        return fail(TS_ERR_SHAPE, "vocab %d outside [1, 2^20]", cfg->vocab);
+    const auto known = [](int t) { return t == TS_LOGITS_F32 || t == TS_LOGITS_BF16; };
+    if (!known(cfg->logits_type) || !known(cfg->out_type))
+        return fail(TS_ERR_ARG, "logits_type %d or out_type %d unknown", cfg->logits_type, cfg->out_type);
+    const int64_t most = 1LL << 40;
+    if (cfg->row_stride < cfg->vocab || cfg->row_stride > most || cfg->out_stride < cfg->vocab || cfg->out_stride > most)
+        return fail(TS_ERR_ARG, "row_stride %lld or out_stride %lld below vocab, or above 2^40", (long long)cfg->row_stride,
+                    (long long)cfg->out_stride);
+    const int in_size = cfg->logits_type == TS_LOGITS_F32 ? 4 : 2, out_size = cfg->out_type == TS_LOGITS_F32 ? 4 : 2;
+    if ((uintptr_t)logits % in_size || (uintptr_t)out % out_size)
+        return fail(TS_ERR_ARG, "misaligned logits or out");
+    if (out == logits && (cfg->out_type != cfg->logits_type || cfg->out_stride != cfg->row_stride))
+        return fail(TS_ERR_ARG, "out == logits needs one type and equal strides");
+    const bool penalties = repetition || frequency || presence;
+    if (!tokens && (penalties || lens || prompt_lens))
+        return fail(TS_ERR_NULL, "penalties and lengths need tokens");
+    if (tokens && !lens)
+        return fail(TS_ERR_NULL, "tokens need lens");
+    if (tokens && (cfg->max_tokens < 0 || cfg->max_tokens > (1 << 30) || cfg->token_stride < cfg->max_tokens ||
+                   cfg->token_stride > most))
+        return fail(TS_ERR_ARG, "max_tokens %d outside [0, 2^30], or token_stride %lld below it or above 2^40",
+                    cfg->max_tokens, (long long)cfg->token_stride);
+    if (!bias_starts != !bias_tokens || !bias_starts != !bias_values)
+        return fail(TS_ERR_NULL, "biases need starts, tokens and values");
+    if (bias_starts && (cfg->num_biases < 0 || cfg->num_biases > (1 << 30)))
+        return fail(TS_ERR_ARG, "num_biases %d outside [0, 2^30]", cfg->num_biases);
+    if (allowed && (cfg->allowed_stride < (cfg->vocab + 31) / 32 || cfg->allowed_stride > most))
+        return fail(TS_ERR_ARG, "allowed_stride %lld below vocab / 32, or above 2^40", (long long)cfg->allowed_stride);
+    if (((uintptr_t)tokens | (uintptr_t)lens | (uintptr_t)prompt_lens | (uintptr_t)repetition | (uintptr_t)frequency |
+         (uintptr_t)presence | (uintptr_t)bias_starts | (uintptr_t)bias_tokens | (uintptr_t)bias_values | (uintptr_t)allowed) & 3)
+        return fail(TS_ERR_ARG, "misaligned pointer (4 B needed)");
+    int st = check_device();
+    if (st)
+        return st;
+    RulesParams p;
+    p.logits = logits;
+    p.out = out;
+    p.tokens = penalties && cfg->max_tokens > 0 ? tokens : nullptr;
+    p.lens = lens;
+    p.prompt_lens = prompt_lens;
+    p.repetition = repetition;
+    p.frequency = frequency;
+    p.presence = presence;
+    p.bias_starts = bias_starts;
+    p.bias_tokens = bias_starts && cfg->num_biases > 0 ? bias_tokens : nullptr;
+    p.bias_values = bias_values;
+    p.allowed = allowed;
+    p.row_stride = cfg->row_stride;
+    p.out_stride = cfg->out_stride;
+    p.token_stride = cfg->token_stride;
+    p.allowed_stride = cfg->allowed_stride;
+    p.vocab = cfg->vocab;
+    p.slices = (cfg->vocab + kSlice - 1) / kSlice;
+    p.max_tokens = cfg->max_tokens;
+    p.num_biases = cfg->num_biases;
+    p.in_place = out == logits;
+    const bool f_in = cfg->logits_type == TS_LOGITS_F32, f_out = cfg->out_type == TS_LOGITS_F32;
+    const auto kernel = f_in ? f_out ? logit_rules_kernel<float, float> : logit_rules_kernel<float, uint16_t>
+                             : f_out ? logit_rules_kernel<uint16_t, float> : logit_rules_kernel<uint16_t, uint16_t>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(cfg->num_seqs * p.slices)), dim3(kThreads),
+                       kSlice * sizeof(uint32_t) * (p.bias_tokens ? 2 : 1), reinterpret_cast<hipStream_t>(stream), p);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? TS_OK : hip_fail(e, "logit rules launch");
+}
+
+}  // extern "C"
