@@ -434,6 +434,19 @@ int ts_rope_append_kv8(const ts_chunk_shape *shape, const ts_rope_config *cfg, c
                        const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts,
                        const float *inv_freq, const void *q_norm, const void *k_norm, void *stream);
 
+/* ts_decode_attn over the cache held in 8 bits: its definition on the cached values,
+ * float32 sums, weights rounded to bf16 as there.  Shape (TS_VARIANT_AUTO or _WAVE),
+ * lengths, workspace contract and errors are those of ts_decode_attn, and one
+ * workspace serves both calls if it is large enough for each.  Codes behind a
+ * sequence's last token, and NaN codes of keys and values that a row does not
+ * see, do not enter its result. */
+size_t ts_decode_attn_kv8_workspace_size(const ts_attn_shape *shape);
+
+int ts_decode_attn_kv8(const ts_attn_shape *shape, const void *q, const void *k_pages, const void *v_pages,
+                       const void *kv_scales, const int32_t *page_table, const int32_t *ctx_lens,
+                       const int32_t *q_lens, void *out, float scale, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
 /* ---- rules on logits -------------------------------------------------------------
  * What a request asks of its row of logits before ts_sample draws from it:
  * penalties for tokens that its text holds, biases and a grammar's mask.  For

@@ -96,7 +96,7 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
            "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn",
            "ts_sample_workspace_size", "ts_sample",
-           "ts_rope_append_kv8", "ts_logit_rules"]
+           "ts_rope_append_kv8", "ts_decode_attn_kv8_workspace_size", "ts_decode_attn_kv8", "ts_logit_rules"]
 
 
 def _load() -> ctypes.CDLL:
@@ -175,6 +175,10 @@ def _load() -> ctypes.CDLL:
     lib.ts_sample.restype = ctypes.c_int
     lib.ts_rope_append_kv8.argtypes = [pchunk, ctypes.POINTER(RopeConfig)] + [P] * 14
     lib.ts_rope_append_kv8.restype = ctypes.c_int
+    lib.ts_decode_attn_kv8_workspace_size.argtypes = [pshape]
+    lib.ts_decode_attn_kv8_workspace_size.restype = SZ
+    lib.ts_decode_attn_kv8.argtypes = [pshape, P, P, P, P, P, P, P, P, ctypes.c_float, P, SZ, P]
+    lib.ts_decode_attn_kv8.restype = ctypes.c_int
     lib.ts_logit_rules.argtypes = [ctypes.POINTER(RulesConfig)] + [P] * 13
     lib.ts_logit_rules.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
@@ -650,6 +654,39 @@ def rope_append_kv8(q, k, v, q_out, k_pages, v_pages, kv_scales, page_table, ctx
                                  q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), kv_scales.data_ptr(),
                                  page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(), _ptr(inv_freq),
                                  _ptr(q_norm), _ptr(k_norm), _stream_ptr(stream)), "ts_rope_append_kv8")
+
+
+def decode_kv8_workspace_size(shape: AttnShape) -> int:
+    n = lib.ts_decode_attn_kv8_workspace_size(ctypes.byref(shape))
+    if n == 0:
+        raise TsError(-2, "ts_decode_attn_kv8_workspace_size")
+    return int(n)
+
+
+def decode_attn_kv8(q, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_lens, out, scale: float, workspace=None,
+                    max_ctx_len: Optional[int] = None, num_workers: int = 0, stream=None, variant: int = 0):
+    """ts_decode_attn_kv8 on torch tensors: as decode_attn (q, out bf16 [B][Qmax][Hq][D]),
+    with pages float8_e4m3fn and kv_scales float8_e8m0fnu [num_pages][Hkv][2]; returns
+    the workspace tensor used."""
+    _check_scales(kv_scales, k_pages)
+    for name, t, dt in (("q", q, _BF16), ("out", out, _BF16), ("k_pages", k_pages, _E4M3), ("v_pages", v_pages, _E4M3),
+                        ("page_table", page_table, _I32), ("ctx_lens", ctx_lens, _I32), ("q_lens", q_lens, _I32)):
+        if t.dtype is not dt or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} tensor")
+    if q.dim() != 4 or out.shape != q.shape or k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+        raise ValueError("out must match q [B][Qmax][Hq][D], and v_pages k_pages [num_pages][Hkv][16][D]")
+    B, D = q.shape[0], q.shape[3]
+    if page_table.dim() != 2 or page_table.shape[0] != B or ctx_lens.shape != (B,) or q_lens.shape != (B,) or k_pages.shape[3] != D:
+        raise ValueError("page_table must be [B][max_pages], ctx_lens and q_lens [B], and head_dim that of the pages")
+    _check_device(q, out, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_lens, workspace, stream=stream)
+    shape = shape_of(q, k_pages, page_table, max_ctx_len, num_workers, variant)
+    if workspace is None:
+        workspace = _own_workspace(decode_kv8_workspace_size(shape), q.device, stream, zeros=True)
+    check(lib.ts_decode_attn_kv8(ctypes.byref(shape), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                 kv_scales.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(), q_lens.data_ptr(),
+                                 out.data_ptr(), scale, workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream)),
+          "ts_decode_attn_kv8")
+    return workspace
 
 
 # ---- rules on logits, sampling ---------------------------------------------------

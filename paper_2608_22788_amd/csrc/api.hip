@@ -24,6 +24,8 @@ namespace tsattn {
 kernel_fn decode_q1_variant(int D, int G);
 kernel_fn verify_variant(int D, int NB);
 kernel_fn verify_group_variant(int D, int NB, int *lds_bytes);
+kernel_fn verify_kv8_variant(int D, int NB);
+kernel_fn verify_group_kv8_variant(int D, int NB, int *lds_bytes);
 kernel_fn verify_team_variant(int rows, int *lds_bytes, int *nbe);
 kernel_fn merge_variant(int D, bool few);
 int debug_check(const ts_attn_shape *s, const int32_t *page_table, const int32_t *ctx_lens,
@@ -77,6 +79,7 @@ struct Plan {
     bool q1;          // one-token VALU kernel, else a matrix-core verify kernel
     bool team;        // verify by four-wavefront teams sharing pages in LDS (head_dim 128)
     bool group;       // single-wavefront streams in groups of four that share splits in LDS
+    bool kv8;         // the cache is held in 8 bits
     bool auto_w;      // worker count chosen by the library (W is then an upper bound)
     int G, NB, rows_per_unit, W;
     size_t ws_cnt_off, ws_dbg_off, ws_o_off, ws_lse_off, ws_bytes;
@@ -214,10 +217,13 @@ int check_shape(const ts_attn_shape *s) {
     return TS_OK;
 }
 
-int make_plan(const ts_attn_shape *s, Plan *pl) {
+int make_plan(const ts_attn_shape *s, bool kv8, Plan *pl) {
     const int st = check_shape(s);
     if (st)
         return st;
+    if (kv8 && s->variant != TS_VARIANT_AUTO && s->variant != TS_VARIANT_WAVE)
+        return fail(TS_ERR_SHAPE, "variant %d does not read a cache held in 8 bits", s->variant);
+    pl->kv8 = kv8;
     const int G = s->num_q_heads / s->num_kv_heads;
     pl->G = G;
     // The one-token VALU kernel runs only on request: the single-wavefront
@@ -232,7 +238,7 @@ int make_plan(const ts_attn_shape *s, Plan *pl) {
     // 20-24 rows at 4-512 sequences: 3-7 % ahead of the team kernel); from
     // three row blocks on the team kernel, which shares each page through LDS
     // (block-draft workload, 64 rows: 12 % ahead at 4 sequences).
-    pl->team = !pl->q1 && s->head_dim == 128 &&
+    pl->team = !pl->q1 && !kv8 && s->head_dim == 128 &&
                (s->variant == TS_VARIANT_TEAM || (s->variant == TS_VARIANT_AUTO && pl->NB >= 3));
     pl->auto_w = s->num_workers == 0;
     // Everything else streams with single wavefronts, grouped four to a worker
@@ -308,11 +314,11 @@ static int finish_plan(const ts_attn_shape *s, Plan &pl, Launch &L) {
         L.main_threads = 4 * kWave;
     } else if (pl.group) {
         int extra = 0;
-        L.main_k = verify_group_variant(D, pl.NB, &extra);
+        L.main_k = pl.kv8 ? verify_group_kv8_variant(D, pl.NB, &extra) : verify_group_variant(D, pl.NB, &extra);
         L.main_lds = ((L.lds + 15) & ~(size_t)15) + (size_t)extra;
         L.main_threads = kGroupWaves * kWave;
     } else {
-        L.main_k = verify_variant(D, pl.NB);
+        L.main_k = pl.kv8 ? verify_kv8_variant(D, pl.NB) : verify_variant(D, pl.NB);
     }
     if (!L.main_k || !merge_variant(D, false))
         return fail(TS_ERR_UNSUPPORTED, "no kernel for head_dim %d, G %d, rows %d", D, pl.G, pl.rows_per_unit);
@@ -403,14 +409,16 @@ static int finish_plan(const ts_attn_shape *s, Plan &pl, Launch &L) {
 }
 
 int launch_attn(const ts_attn_shape *s, const void *q, const void *k_pages, const void *v_pages,
-                  const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_lens,
+                  const void *kv_scales, bool kv8, const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_lens,
                   void *out, float scale, void *workspace, size_t workspace_bytes, void *stream,
                   void *ev_begin, void *ev_end, int merge_polls) {
     clear_error();
     Plan pl;
-    int st = make_plan(s, &pl);
+    int st = make_plan(s, kv8, &pl);
     if (st)
         return st;
+    if (kv8 && !kv_scales)
+        return fail(TS_ERR_NULL, "kv_scales is NULL");
     if (!q || !k_pages || !v_pages || !page_table || !ctx_lens || !q_lens || !out)
         return fail(TS_ERR_NULL, "a tensor pointer is NULL");
     if (!workspace)
@@ -418,7 +426,7 @@ int launch_attn(const ts_attn_shape *s, const void *q, const void *k_pages, cons
     if (workspace_bytes < pl.ws_bytes)
         return fail(TS_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, pl.ws_bytes);
     if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)out & 15) ||
-        ((uintptr_t)k_pages & 15) || ((uintptr_t)v_pages & 15))
+        ((uintptr_t)k_pages & 15) || ((uintptr_t)v_pages & 15) || (kv8 && ((uintptr_t)kv_scales & 15)))
         return fail(TS_ERR_ARG, "misaligned pointer (workspace needs 256 B, tensors 16 B)");
     if (!std::isfinite(scale))
         return fail(TS_ERR_ARG, "scale is not finite");
@@ -463,6 +471,7 @@ int launch_attn(const ts_attn_shape *s, const void *q, const void *k_pages, cons
     p.cnt_shift = (int8_t)L.cnt_shift;
     p.merge_polls = (int16_t)merge_polls;
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.kv_scales = static_cast<const uint8_t *>(kv_scales);
 
     hipError_t e;
     if (ev_begin || ev_end) {
@@ -495,7 +504,15 @@ extern "C" {
 size_t ts_decode_attn_workspace_size(const ts_attn_shape *shape) {
     clear_error();
     Plan pl;
-    if (make_plan(shape, &pl))
+    if (make_plan(shape, false, &pl))
+        return 0;
+    return pl.ws_bytes;
+}
+
+size_t ts_decode_attn_kv8_workspace_size(const ts_attn_shape *shape) {
+    clear_error();
+    Plan pl;
+    if (make_plan(shape, true, &pl))
         return 0;
     return pl.ws_bytes;
 }
@@ -506,7 +523,7 @@ int ts_decode_attn_plan(const ts_attn_shape *shape, ts_attn_plan *plan) {
         if (!plan)
             return fail(TS_ERR_NULL, "plan is NULL");
         Plan pl;
-        int st = make_plan(shape, &pl);
+        int st = make_plan(shape, false, &pl);
         if (st)
             return st;
         Launch L;
@@ -534,7 +551,7 @@ int ts_decode_attn(const ts_attn_shape *shape, const void *q, const void *k_page
                    const int32_t *q_lens, void *out, float scale, void *workspace,
                    size_t workspace_bytes, void *stream) {
     try {
-        return launch_attn(shape, q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale,
+        return launch_attn(shape, q, k_pages, v_pages, nullptr, false, page_table, ctx_lens, q_lens, out, scale,
                       workspace, workspace_bytes, stream, nullptr, nullptr, kMergePolls);
     } catch (...) {
         return fail(TS_ERR_HIP, "unexpected C++ exception");
@@ -547,7 +564,7 @@ int ts_decode_attn_events(const ts_attn_shape *shape, const void *q, const void 
                           float scale, void *workspace, size_t workspace_bytes, void *stream,
                           void *ev_begin, void *ev_end) {
     try {
-        return launch_attn(shape, q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale,
+        return launch_attn(shape, q, k_pages, v_pages, nullptr, false, page_table, ctx_lens, q_lens, out, scale,
                       workspace, workspace_bytes, stream, ev_begin, ev_end, kMergePolls);
     } catch (...) {
         return fail(TS_ERR_HIP, "unexpected C++ exception");
@@ -560,8 +577,20 @@ int ts_decode_attn_polls(const ts_attn_shape *shape, const void *q, const void *
                          float scale, void *workspace, size_t workspace_bytes, void *stream,
                          int32_t merge_polls) {
     try {
-        return launch_attn(shape, q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale,
+        return launch_attn(shape, q, k_pages, v_pages, nullptr, false, page_table, ctx_lens, q_lens, out, scale,
                       workspace, workspace_bytes, stream, nullptr, nullptr, merge_polls);
+    } catch (...) {
+        return fail(TS_ERR_HIP, "unexpected C++ exception");
+    }
+}
+
+int ts_decode_attn_kv8(const ts_attn_shape *shape, const void *q, const void *k_pages, const void *v_pages,
+                       const void *kv_scales, const int32_t *page_table, const int32_t *ctx_lens,
+                       const int32_t *q_lens, void *out, float scale, void *workspace, size_t workspace_bytes,
+                       void *stream) {
+    try {
+        return launch_attn(shape, q, k_pages, v_pages, kv_scales, true, page_table, ctx_lens, q_lens, out, scale,
+                           workspace, workspace_bytes, stream, nullptr, nullptr, kMergePolls);
     } catch (...) {
         return fail(TS_ERR_HIP, "unexpected C++ exception");
     }

@@ -51,7 +51,7 @@ constexpr int kCombineInLaunch = 2;  // merge workgroups after the W workers of 
 // overlapping calls can cause.
 constexpr int kMergePolls = 8192;
 
-struct AttnParams {   // 128 bytes of kernel arguments
+struct AttnParams {   // 136 bytes of kernel arguments
     const uint16_t *q;          // [B][Qmax][Hq][D] bf16
     const uint16_t *k_pages;    // [num_pages][Hkv][P][D] bf16
     const uint16_t *v_pages;
@@ -72,6 +72,7 @@ struct AttnParams {   // 128 bytes of kernel arguments
     int8_t cnt_shift;           // log2 of the ints between the counters of consecutive units
     int16_t merge_polls;        // polls a merge wavefront waits before it leaves its row to the last worker
     float scale_log2;           // scale * log2(e)
+    const uint8_t *kv_scales;   // [num_pages][Hkv][2] (the cache held in 8 bits, whose pages hold bytes)
 };
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));

@@ -81,7 +81,7 @@ extern "C" int ts_decode_attn_noalloc(const ts_attn_shape *shape, const void *q,
         st = scratch_address(&ws);
         if (st)
             return st;
-        return launch_attn(shape, q, k_pages, v_pages, page_table, ctx_lens, q_lens, out, scale, ws,
+        return launch_attn(shape, q, k_pages, v_pages, nullptr, false, page_table, ctx_lens, q_lens, out, scale, ws,
                            kScratchBytes, stream, nullptr, nullptr, kMergePolls);
     } catch (...) {
         return fail(TS_ERR_HIP, "unexpected C++ exception");

@@ -8,6 +8,7 @@ import torch
 
 from oracle import kv8
 from paper_2608_22788_amd import binding as b
+from test_abi import base_shape
 from test_chunk import BAD_SHAPES, config, shape
 
 
@@ -34,6 +35,50 @@ def test_append_arguments_rejected():
         assert append(s, config(**kw)) == -6, kw
     assert append(s, config(eps=float("nan")), qn=16) == -6
     assert append(shape(num_tokens=0, max_q_len=0), None, q=None, scales=None) == 0
+
+
+def decode(s, q=16, k=16, v=16, scales=16, table=16, ctx=16, ql=16, out=16, scale=0.125, ws=256, nbytes=1 << 40):
+    return b.lib.ts_decode_attn_kv8(ctypes.byref(s) if s else None, q, k, v, scales, table, ctx, ql, out,
+                                    ctypes.c_float(scale), ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", [dict(num_seqs=0), dict(num_q_heads=6, num_kv_heads=4), dict(head_dim=96),
+                                dict(max_q_len=17), dict(num_q_heads=32, num_kv_heads=1, max_q_len=4),
+                                dict(max_ctx_len=257), dict(num_pages=0), dict(num_workers=-1)], ids=str)
+def test_decode_bad_shapes_rejected(kw):
+    s = base_shape(**kw)
+    assert b.lib.ts_decode_attn_kv8_workspace_size(ctypes.byref(s)) == 0 and decode(s) == -2
+
+
+def test_decode_arguments_rejected():
+    s = base_shape()
+    need = b.decode_kv8_workspace_size(s)
+    assert need > 0 and need % 256 == 0
+    assert decode(None) == -1
+    for name in ("q", "k", "v", "scales", "table", "ctx", "ql", "out", "ws"):
+        assert decode(s, **{name: None}) == -1, name
+    assert decode(s, nbytes=need - 1) == -3
+    for kw in (dict(ws=128), dict(q=8), dict(k=24), dict(v=2), dict(scales=8), dict(out=8), dict(scale=float("nan"))):
+        assert decode(s, **kw) == -6, kw
+    for variant in (b.VARIANT_TEAM, b.VARIANT_VALU, 7):
+        s = base_shape(head_dim=128)
+        s.variant = variant
+        assert decode(s) == -2 and b.lib.ts_decode_attn_kv8_workspace_size(ctypes.byref(s)) == 0
+
+
+def test_decode_binding_refuses_other_tensors():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    pages = torch.zeros(5, 2, 16, 64).to(torch.float8_e4m3fn)
+    good = dict(q=torch.zeros(3, 2, 4, 64, dtype=torch.bfloat16), k_pages=pages, v_pages=pages,
+                kv_scales=torch.zeros(5, 2, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu), page_table=i32(3, 2),
+                ctx_lens=i32(3), q_lens=i32(3), out=torch.zeros(3, 2, 4, 64, dtype=torch.bfloat16), scale=1.0)
+    for name, bad in (("q", good["q"].float()), ("q", good["q"][:, :, ::2]), ("k_pages", pages.float()),
+                      ("v_pages", pages[:4]), ("kv_scales", good["kv_scales"][:2]), ("page_table", i32(2, 2)),
+                      ("ctx_lens", i32(4)), ("q_lens", i32(3, 1)), ("out", good["out"][:2])):
+        with pytest.raises(ValueError, match=name):
+            b.decode_attn_kv8(**{**good, name: bad})
+    with pytest.raises(ValueError, match="CUDA"):
+        b.decode_attn_kv8(**good)
 
 
 def test_binding_refuses_other_types():
