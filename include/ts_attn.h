@@ -408,7 +408,9 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *                     aligned
  *   kv_scales         uint8 [num_pages][num_kv_heads][2], 16-byte aligned: the
  *                     biased exponents (e8m0) of a power of two for the keys and
- *                     one for the values of each page and KV head
+ *                     one for the values of each page and KV head (where the last
+ *                     pair ends in the middle of an aligned word of 4 bytes,
+ *                     ts_chunk_attn_kv8 reads the whole word)
  * A cached value is code * 2^(byte - 127), exactly a bf16 number for the bytes 27
  * to 227 that ts_rope_append_kv8 writes (the powers 2^-100 to 2^100); with others
  * the product is taken as bf16 takes it.  Code 0x7f (and 0xff) is NaN; e4m3 has no
@@ -446,6 +448,17 @@ int ts_decode_attn_kv8(const ts_attn_shape *shape, const void *q, const void *k_
                        const void *kv_scales, const int32_t *page_table, const int32_t *ctx_lens,
                        const int32_t *q_lens, void *out, float scale, void *workspace, size_t workspace_bytes,
                        void *stream);
+
+/* ts_chunk_attn over the cache held in 8 bits: its definition on the cached values.
+ * Shape, lengths, strides, workspace contract and errors are those of
+ * ts_chunk_attn; a page outside the pool reads as zeros, and keys and values that a
+ * row does not see do not enter its result, also where their codes are NaN. */
+size_t ts_chunk_attn_kv8_workspace_size(const ts_chunk_shape *shape);
+
+int ts_chunk_attn_kv8(const ts_chunk_shape *shape, const void *q, int64_t q_stride, const void *k_pages,
+                      const void *v_pages, const void *kv_scales, const int32_t *page_table,
+                      const int32_t *ctx_lens, const int32_t *q_starts, void *out, int64_t out_stride, float scale,
+                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- rules on logits -------------------------------------------------------------
  * What a request asks of its row of logits before ts_sample draws from it:

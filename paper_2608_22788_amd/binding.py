@@ -96,7 +96,8 @@ EXPORTS = ["ts_decode_attn_workspace_size", "ts_decode_attn", "ts_decode_attn_ev
            "ts_kv_append", "ts_spec_accept_workspace_size", "ts_spec_accept",
            "ts_rope_append", "ts_chunk_attn_workspace_size", "ts_chunk_attn",
            "ts_sample_workspace_size", "ts_sample",
-           "ts_rope_append_kv8", "ts_decode_attn_kv8_workspace_size", "ts_decode_attn_kv8", "ts_logit_rules"]
+           "ts_rope_append_kv8", "ts_decode_attn_kv8_workspace_size", "ts_decode_attn_kv8",
+           "ts_chunk_attn_kv8_workspace_size", "ts_chunk_attn_kv8", "ts_logit_rules"]
 
 
 def _load() -> ctypes.CDLL:
@@ -179,6 +180,10 @@ def _load() -> ctypes.CDLL:
     lib.ts_decode_attn_kv8_workspace_size.restype = SZ
     lib.ts_decode_attn_kv8.argtypes = [pshape, P, P, P, P, P, P, P, P, ctypes.c_float, P, SZ, P]
     lib.ts_decode_attn_kv8.restype = ctypes.c_int
+    lib.ts_chunk_attn_kv8_workspace_size.argtypes = [pchunk]
+    lib.ts_chunk_attn_kv8_workspace_size.restype = SZ
+    lib.ts_chunk_attn_kv8.argtypes = [pchunk, P, I64, P, P, P, P, P, P, P, I64, ctypes.c_float, P, SZ, P]
+    lib.ts_chunk_attn_kv8.restype = ctypes.c_int
     lib.ts_logit_rules.argtypes = [ctypes.POINTER(RulesConfig)] + [P] * 13
     lib.ts_logit_rules.restype = ctypes.c_int
     lib.ts_status_string.argtypes = [ctypes.c_int]
@@ -686,6 +691,37 @@ def decode_attn_kv8(q, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_lens
                                  kv_scales.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(), q_lens.data_ptr(),
                                  out.data_ptr(), scale, workspace.data_ptr(), _nbytes(workspace), _stream_ptr(stream)),
           "ts_decode_attn_kv8")
+    return workspace
+
+
+def chunk_kv8_workspace_size(shape: ChunkShape) -> int:
+    n = lib.ts_chunk_attn_kv8_workspace_size(ctypes.byref(shape))
+    if n == 0:
+        raise TsError(-2, "ts_chunk_attn_kv8_workspace_size")
+    return int(n)
+
+
+def chunk_attn_kv8(q, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_starts, out, scale: float, workspace=None,
+                   max_q_len: Optional[int] = None, max_ctx_len: Optional[int] = None, num_workers: int = 0,
+                   stream=None):
+    """ts_chunk_attn_kv8 on torch tensors: as chunk_attn (q, out: bf16 [T][Hq][D], rows
+    may be strided), with pages float8_e4m3fn and kv_scales float8_e8m0fnu
+    [num_pages][Hkv][2]; returns the workspace tensor used."""
+    _check_scales(kv_scales, k_pages)
+    T, Hq, D, q_stride = _rows(q, "q")
+    To, Ho, Do, out_stride = _rows(out, "out")
+    NP, Hkv, P, Dp, B, maxp = _paged(k_pages, v_pages, page_table, ctx_lens, q_starts, _E4M3)
+    if not (T == To and Hq == Ho and D == Do == Dp):
+        raise ValueError("out must match q, and head_dim that of the pages")
+    _check_device(q, out, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_starts, workspace, stream=stream)
+    shape = ChunkShape(B, T, Hq, Hkv, D, P, T if max_q_len is None else int(max_q_len), maxp,
+                       maxp * P if max_ctx_len is None else int(max_ctx_len), num_workers, NP)
+    if workspace is None:
+        workspace = _own_workspace(chunk_kv8_workspace_size(shape), q.device, stream)
+    check(lib.ts_chunk_attn_kv8(ctypes.byref(shape), q.data_ptr(), q_stride, k_pages.data_ptr(), v_pages.data_ptr(),
+                                kv_scales.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(), q_starts.data_ptr(),
+                                out.data_ptr(), out_stride, scale, workspace.data_ptr(), _nbytes(workspace),
+                                _stream_ptr(stream)), "ts_chunk_attn_kv8")
     return workspace
 
 

@@ -61,6 +61,7 @@
 #include "attn_common.h"
 #include "chunk_common.h"
 #include "chunk_partition.h"
+#include "kv8_common.h"
 #include "ts_attn.h"
 #include "ts_internal.h"
 
@@ -73,7 +74,11 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRowBlock = 32;      // rows of a matrix-core tile
 constexpr int kChunkWaves = 8;
-constexpr int kStages = 4;         // KV tiles in LDS: one in use, the others on their way
+// KV tiles in LDS: one in use, the others on their way.  Of the cache held in 8
+// bits: as bf16, one whose values are in use, one whose keys are, one being
+// converted; and as codes, on their way.  Both take 128 KiB at head_dim 128.
+constexpr int stages(bool k8) { return k8 ? 3 : 4; }
+constexpr int kCodeStages = 2;
 static_assert(kTileRows == kChunkWaves * kRowBlock, "a row block per wavefront");
 constexpr float kTiny = 1.17549435e-38f;   // the smallest normal float32
 constexpr float kLowest = -3.0e38f;       // the reference of a row without a score yet
@@ -97,6 +102,7 @@ struct ChunkParams {
     uint32_t range_inv;
     float scale_log2;           // |scale| * log2(e)
     uint32_t q_sign;            // sign bits to flip in a pair of q values
+    const uint8_t *kv_scales;   // [num_pages][Hkv][2] (the cache held in 8 bits, whose pages hold bytes)
 };
 
 // Sequence b: its first packed row, new tokens and tokens in front of them.
@@ -272,7 +278,7 @@ typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 // whose row tiles find each other's keys in the L2, would take 588 instead of 519.
 template <int kLoads, bool kOnce>
 __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int from, int twist) {
-    static_assert(kLoads == 2 || kLoads == 4, "blocks");
+    static_assert(kLoads == 1 || kLoads == 2 || kLoads == 4, "blocks");
 #define TS_DMA_BLOCK(reg, offset, kept) "buffer_load_dwordx4 %" reg ", %1, 0 offen offset:" offset kept " lds\n\t"
 #define TS_DMA_BLOCKS(kept)                                                                                            \
     if constexpr (kLoads == 4)                                                                                         \
@@ -280,9 +286,12 @@ __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int f
                          TS_DMA_BLOCK("4", "2048", kept) TS_DMA_BLOCK("5", "%6", kept)::"s"(to), "s"(rsrc), "v"(from), \
                      "v"(from ^ twist), "v"(from ^ 2 * twist), "v"(from ^ 3 * twist), "n"(3 * 1024)                    \
                      : "m0", "memory");                                                                                \
-    else                                                                                                               \
+    else if constexpr (kLoads == 2)                                                                                    \
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept)                                   \
                          TS_DMA_BLOCK("3", "1024", kept)::"s"(to), "s"(rsrc), "v"(from), "v"(from ^ twist)             \
+                     : "m0", "memory");                                                                                \
+    else                                                                                                               \
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" TS_DMA_BLOCK("2", "0", kept)::"s"(to), "s"(rsrc), "v"(from)    \
                      : "m0", "memory")
     // (a clobber of m0 warns that its value is not kept: nobody needs it)
 #pragma clang diagnostic push
@@ -299,7 +308,7 @@ __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int f
 // Waits until at most the loads of the last `later` tiles are under way.
 template <int kLoads>
 __device__ __forceinline__ void dma_wait(int later) {
-    static_assert(kStages == 4, "up to two later tiles");
+    static_assert(stages(false) == 4 && kCodeStages == 2, "up to two later tiles");
     if (later >= 2)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
     else if (later == 1)
@@ -308,14 +317,18 @@ __device__ __forceinline__ void dma_wait(int later) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-template <int D>
+template <int D, bool k8>
 struct Chunk {
+    static constexpr int kStages = stages(k8);
     static constexpr int kRowBytes = 2 * D;
     static constexpr int kPieces = kRowBytes / 16;         // 16-byte pieces of a row
     static constexpr int kKBytes = kKeyTile * kRowBytes;   // the keys of a stage; the values follow
     static constexpr int kStage = 2 * kKBytes;
-    static constexpr int kLds = kStages * kStage;
-    static constexpr int kLoads = kPage * kRowBytes / (16 * kWave);   // loads of a wave per page block
+    static constexpr int kCodeBytes = k8 ? 2 * kKeyTile * D : 0;   // keys and values of a tile as codes
+    static constexpr int kCodes = kStages * kStage;        // where they begin
+    static constexpr int kLds = kCodes + kCodeStages * kCodeBytes;
+    static constexpr int kPageBytes = k8 ? kPage * D : kPage * kRowBytes;   // of one (page, KV head) block in memory
+    static constexpr int kLoads = kPageBytes / (16 * kWave);   // loads of a wave per page block
     static constexpr int kKSteps = D / 16;
     static constexpr int kDTiles = D / 32;
 
@@ -338,25 +351,82 @@ struct Chunk {
         int from, twist;          // and where in a page it loads from (dma_blocks)
     };
 
+    // The power of a wavefront's page, read as a scalar: the aligned word that holds
+    // its two bytes, and where in it this wavefront's is.
+    struct Power {
+        uint32_t word;
+        int shift;
+        __device__ __forceinline__ float value() const { return power_of(word >> shift & 0xff); }
+    };
+
     // Starts loading a wavefront's part of a tile, the keys (wavefronts 0 to 3)
-    // or values of a page.  A page outside the pool is stored as zeros; what is
-    // under way then arrives first, so that counts of loads stay counts of tiles.
-    __device__ __forceinline__ static void dma_page(const ChunkParams &p, const State &st, int pid, bool once, int g, char *stage, int wave, int lane) {
-        char *to = stage + wave * (kPage * kRowBytes);   // (the values follow the keys)
+    // or values of a page, to `stage`.  A page outside the pool is stored as zeros;
+    // what is under way then arrives first, so that counts of loads stay counts of
+    // tiles.
+    __device__ __forceinline__ static Power dma_page(const ChunkParams &p, const State &st, int pid, bool once, int g, char *stage, int wave, int lane) {
+        char *to = stage + wave * kPageBytes;   // (the values follow the keys)
+        Power power = {0x7f7f7f7fu, 0};
         if (__builtin_expect(pid < 0 || pid >= p.num_pages, 0)) {
             dma_wait<kLoads>(0);
 #pragma unroll
             for (int i = 0; i < kLoads; i++)
                 *reinterpret_cast<u32x4_t *>(to + 16 * (i * kWave + lane)) = u32x4_t{0u, 0u, 0u, 0u};
-            return;
+            return power;
         }
-        const size_t base = ((size_t)pid * p.Hkv + g) * (size_t)(kPage * D);
-        const block_rsrc_t rsrc = block_rsrc((wave < kTilePages ? p.k_pages : p.v_pages) + base, kPage * kRowBytes);
+        const size_t block = (size_t)pid * p.Hkv + g;
+        const char *pages = reinterpret_cast<const char *>(wave < kTilePages ? p.k_pages : p.v_pages);
+        if constexpr (k8) {
+            power.word = (uint32_t)ld_meta(reinterpret_cast<const int32_t *>(p.kv_scales), block / 2);
+            power.shift = 16 * (int)(block % 2) + (wave < kTilePages ? 0 : 8);
+        }
+        const block_rsrc_t rsrc = block_rsrc(pages + block * kPageBytes, kPageBytes);
         const uint32_t at = (uint32_t)first_lane_int((int)(uintptr_t)(lds_char *)to);
         if (once)
             dma_blocks<kLoads, true>(rsrc, at, st.from, st.twist);
         else
             dma_blocks<kLoads, false>(rsrc, at, st.from, st.twist);
+        return power;
+    }
+
+    // A wavefront's page of a tile from codes to bf16, times its power (exact), in the
+    // order in which rows are stored: a lane takes back the 16 codes that it loaded,
+    // two pieces of a row.  NaN codes of values in `rows` rows (kClean) are replaced by
+    // zero; returns whether one of the first `rows` rows held one (clean_page).
+    __device__ __forceinline__ static bool convert_page(char *lds, int codes, int stage, float power, bool clean, int rows, int wave, int lane) {
+        constexpr int kLanes = D / 16;   // lanes of a row
+        const char *from = lds + kCodes + codes * kCodeBytes + wave * kPageBytes + 16 * lane;
+        char *to = lds + stage * kStage + wave * (kPage * kRowBytes);
+        const int piece = 2 * (lane % kLanes);
+        bool any = false;
+        u32x4_t c[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            c[i] = *reinterpret_cast<const u32x4_t *>(from + 1024 * i);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int row = i * (kWave / kLanes) + lane / kLanes;
+            if (__builtin_expect(clean, 0)) {
+                uint32_t odd = 0;
+#pragma unroll
+                for (int w = 0; w < 4; w++) {
+                    const uint32_t m = ((c[i][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    c[i][w] &= ~((m >> 7) * 0xffu);
+                    odd |= m;
+                }
+                any |= odd && row < rows;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                u32x4_t x;
+#pragma unroll
+                for (int w = 0; w < 4; w++)
+                    x[w] = __builtin_bit_cast(uint32_t, w % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i][2 * u + w / 2], power, true)
+                                                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i][2 * u + w / 2], power, false));
+                const int at = wave < kTilePages ? k_piece(row, piece + u) : v_piece(row, piece + u);
+                *reinterpret_cast<u32x4_t *>(to + row * kRowBytes + 16 * at) = x;
+            }
+        }
+        return any;
     }
 
     __device__ __forceinline__ static void set_addresses(State &st, char *lds, int wave, int lane) {
@@ -372,10 +442,11 @@ struct Chunk {
         // Block i of 1 KiB of a page holds its rows (64 / kPieces) i + lane /
         // kPieces in stored order: the exchange of key pieces differs by 4 i,
         // 64 i bytes, that of value pieces not at all.
+        // (Codes are loaded in the order of the page.)
         const int row = lane / kPieces, piece = lane % kPieces;
         const bool keys = wave < kTilePages;
-        st.from = row * kRowBytes + 16 * (keys ? k_piece(row, piece) : v_piece(row, piece));
-        st.twist = keys ? 64 : 0;
+        st.from = k8 ? 16 * lane : row * kRowBytes + 16 * (keys ? k_piece(row, piece) : v_piece(row, piece));
+        st.twist = keys && !k8 ? 64 : 0;
     }
 
     // Keys 32 kt .. + 31, dimensions 16 ks .. + 15.
@@ -564,9 +635,24 @@ struct Chunk {
             const int pid = ld_meta(pt, t / kPage);
             if (pid < 0 || pid >= p.num_pages)
                 continue;
-            const uint16_t *row = p.v_pages + (((size_t)pid * p.Hkv + g) * kPage + t % kPage) * D + 4 * h;
+            const size_t at = (((size_t)pid * p.Hkv + g) * kPage + t % kPage) * D + 4 * h;
             if (t >= st.lim)
                 continue;
+            if constexpr (k8) {
+                const uint8_t *row = reinterpret_cast<const uint8_t *>(p.v_pages) + at;
+#pragma unroll
+                for (int dt = 0; dt < kDTiles; dt++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t x = *reinterpret_cast<const uint32_t *>(row + 32 * dt + 8 * e);
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            if ((x >> 8 * i & 0x7f) == 0x7f)
+                                st.o[dt][4 * e + i] = __uint_as_float(0x7fc00000u);
+                    }
+                continue;
+            }
+            const uint16_t *row = p.v_pages + at;
 #pragma unroll
             for (int dt = 0; dt < kDTiles; dt++)
 #pragma unroll
@@ -587,6 +673,7 @@ struct Chunk {
         int first, last;   // page of the first tile; the last page of the context
         bool once;         // no other row tile reads them
         int ids[4];
+        Power power[kCodeStages];   // of the tiles on their way
         __device__ __forceinline__ int next(int i) {   // tiles i = 0, 1, ... of the piece, in order
             if (i % 4 == 0)
 #pragma unroll
@@ -601,10 +688,17 @@ struct Chunk {
     __device__ __forceinline__ static Pages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
         const SeqInfo sq = seq_info(p, pc.b);
         Pages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
-                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}};
-        const int n = min(pc.j1 - pc.j0, kStages - 1);
-        for (int i = 0; i < n; i++)
-            dma_page(p, st, pages.next(i), pages.once, pc.g, lds + i * kStage, wave, lane);
+                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}, {}};
+        if constexpr (k8) {
+#pragma unroll
+            for (int i = 0; i < kCodeStages; i++)
+                if (i < pc.j1 - pc.j0)
+                    pages.power[i] = dma_page(p, st, pages.next(i), pages.once, pc.g, lds + kCodes + i * kCodeBytes, wave, lane);
+        } else {
+            const int n = min(pc.j1 - pc.j0, kStages - 1);
+            for (int i = 0; i < n; i++)
+                dma_page(p, st, pages.next(i), pages.once, pc.g, lds + i * kStage, wave, lane);
+        }
         return pages;
     }
 
@@ -667,33 +761,61 @@ struct Chunk {
                     odd |= clean_page(lds + i % kStages * kStage, wave, lane, sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage);
                 lds_barrier();
             };
+            // Codes: tile i becomes bf16 once it is there, and its place is loaded
+            // with tile i + 2.  A wavefront reads only codes that it loaded.
+            const auto convert = [&](int i, int slot) __attribute__((always_inline)) {
+                dma_wait<kLoads>(i + 1 < n ? 1 : 0);
+                const bool clean = i >= n_plain && wave >= kTilePages;
+                odd |= convert_page(lds, slot, i % kStages, pages.power[slot].value(), clean,
+                                    sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage, wave, lane);
+                if (i + kCodeStages < n)
+                    pages.power[slot] = dma_page(p, st, pages.next(i + kCodeStages), pages.once, pc.g,
+                                                 lds + kCodes + slot * kCodeBytes, wave, lane);
+            };
             const auto room = [&](int i) { return st.lim - (pc.j0 + i) * kKeyTile - 4 * h; };
-            const auto advance = [&](int i) __attribute__((always_inline)) {
+            // (i % 2 == slot)
+            const auto advance = [&](int i, int slot) __attribute__((always_inline)) {
+                if constexpr (k8) {
+                    lds_barrier();
+                    if (i + 2 < n)
+                        convert(i + 2, slot);
+                    return;
+                }
                 arrive(i + 1, min(n - 2 - i, 1));
                 if (i + kStages - 1 < n)
                     dma_page(p, st, pages.next(i + kStages - 1), pages.once, pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
-            const auto step = [&](int i, Scores &c, Scores &next) __attribute__((always_inline)) {
-                advance(i);
+            const auto step = [&](int i, int slot, Scores &c, Scores &next) __attribute__((always_inline)) {
+                advance(i, slot);
                 tile_step<true>(p, st, c, next, i % kStages * kStage, (i + 1) % kStages * kStage, i >= n_plain, room(i));
             };
-            arrive(0, min(n - 1, 2));
+            if constexpr (k8) {
+                convert(0, 0);
+                if (n > 1)
+                    convert(1, 1);
+                lds_barrier();
+            } else {
+                arrive(0, min(n - 1, 2));
+            }
             if (__any(row_ok)) {
                 Scores a, b;
                 scores(st, 0, a);
                 largest(p, a);
                 for (int i = 0; i + 1 < n; i += 2) {
-                    step(i, a, b);
+                    step(i, 0, a, b);
                     if (i + 2 >= n) {
                         a = b;
                         break;
                     }
-                    step(i + 1, b, a);
+                    step(i + 1, 1, b, a);
                 }
                 tile_step<false>(p, st, a, b, (n - 1) % kStages * kStage, 0, n > n_plain, room(n - 1));
             } else {   // no row of this wavefront has a token: it only loads
-                for (int i = 0; i + 1 < n; i++)
-                    advance(i);
+                for (int i = 0; i + 1 < n; i += 2) {
+                    advance(i, 0);
+                    if (i + 2 < n)
+                        advance(i + 1, 1);
+                }
             }
             lds_barrier();
             if (n_plain < n) {   // the same for every wavefront
@@ -754,10 +876,10 @@ struct Chunk {
     }
 };
 
-template <int D>
+template <int D, bool k8>
 __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(ChunkParams p) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // the tiles, then the prefix
-    uint64_t *s_tiles = reinterpret_cast<uint64_t *>(lds + Chunk<D>::kLds);
+    uint64_t *s_tiles = reinterpret_cast<uint64_t *>(lds + Chunk<D, k8>::kLds);
     tile_ends(p, s_tiles);
     const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
     const int w = xcd_worker(blockIdx.x, p.W);
@@ -765,7 +887,7 @@ __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(Chun
     const int64_t end = first_lane_int64(range_start(ptot, w + 1, p.W, p.range_inv));
     if (ptot == 0 && w == p.W - 1 && threadIdx.x == 0)
         p.cuts[w].ptot = 0;
-    Chunk<D>::work(p, s_tiles, w, begin, end, lds);
+    Chunk<D, k8>::work(p, s_tiles, w, begin, end, lds);
 }
 
 // Joins the pieces of the units that a worker boundary cuts: workgroup x takes
@@ -927,21 +1049,12 @@ int check_stride(const char *name, int64_t stride, int64_t row) {
     return TS_OK;
 }
 
-}  // namespace tsattn
-
-using namespace tsattn;
-
-extern "C" {
-
-size_t ts_chunk_attn_workspace_size(const ts_chunk_shape *s) {
-    clear_error();
-    ChunkPlan pl;
-    return make_chunk_plan(s, &pl) == TS_OK ? pl.ws_bytes : 0;
-}
-
-int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
-                  const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts, void *out,
-                  int64_t out_stride, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+// ts_chunk_attn and ts_chunk_attn_kv8.
+template <bool k8>
+static int launch_chunk(const ts_chunk_shape *s, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                        const void *kv_scales, const int32_t *page_table, const int32_t *ctx_lens,
+                        const int32_t *q_starts, void *out, int64_t out_stride, float scale, void *workspace,
+                        size_t workspace_bytes, void *stream) {
     clear_error();
     ChunkPlan pl;
     int st = make_chunk_plan(s, &pl);
@@ -951,11 +1064,13 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
         return TS_OK;   // no rows, whose tensors may be NULL
     if (!q || !k_pages || !v_pages || !page_table || !ctx_lens || !q_starts || !out || !workspace)
         return fail(TS_ERR_NULL, "a pointer is NULL");
+    if (k8 && !kv_scales)
+        return fail(TS_ERR_NULL, "kv_scales is NULL");
     if (!std::isfinite(scale))
         return fail(TS_ERR_ARG, "scale must be finite");
     if (workspace_bytes < pl.ws_bytes)
         return fail(TS_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, pl.ws_bytes);
-    if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out) & 15) || ((uintptr_t)workspace & 255))
+    if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out | (uintptr_t)kv_scales) & 15) || ((uintptr_t)workspace & 255))
         return fail(TS_ERR_ARG, "misaligned pointer (tensors 16 B, workspace 256 B)");
     const int64_t row = (int64_t)s->num_q_heads * s->head_dim;
     if ((st = check_stride("q_stride", q_stride, row)) || (st = check_stride("out_stride", out_stride, row)))
@@ -991,13 +1106,14 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
     // masked one)
     p.scale_log2 = std::max(std::fabs(scale) * 1.44269504088896341f, 1e-30f);
     p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
+    p.kv_scales = static_cast<const uint8_t *>(kv_scales);
     const size_t pre = (size_t)s->num_seqs * sizeof(uint64_t);
     const bool small = s->head_dim == 64;
-    const auto main_k = small ? chunk_attn_kernel<64> : chunk_attn_kernel<128>;
+    const auto main_k = small ? chunk_attn_kernel<64, k8> : chunk_attn_kernel<128, k8>;
     const auto merge_k = small ? chunk_merge_kernel<64> : chunk_merge_kernel<128>;
     hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(main_k, dim3((unsigned)pl.W), dim3(kChunkWaves * kWave),
-                       pre + (small ? Chunk<64>::kLds : Chunk<128>::kLds), hs, p);
+                       pre + (small ? Chunk<64, k8>::kLds : Chunk<128, k8>::kLds), hs, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return hip_fail(e, "chunk attention launch");
@@ -1008,6 +1124,35 @@ int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, cons
             return hip_fail(e, "chunk merge launch");
     }
     return TS_OK;
+}
+
+}  // namespace tsattn
+
+using namespace tsattn;
+
+extern "C" {
+
+size_t ts_chunk_attn_workspace_size(const ts_chunk_shape *s) {
+    clear_error();
+    ChunkPlan pl;
+    return make_chunk_plan(s, &pl) == TS_OK ? pl.ws_bytes : 0;
+}
+
+size_t ts_chunk_attn_kv8_workspace_size(const ts_chunk_shape *s) { return ts_chunk_attn_workspace_size(s); }
+
+int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                  const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts, void *out,
+                  int64_t out_stride, float scale, void *workspace, size_t workspace_bytes, void *stream) {
+    return launch_chunk<false>(s, q, q_stride, k_pages, v_pages, nullptr, page_table, ctx_lens, q_starts, out, out_stride,
+                               scale, workspace, workspace_bytes, stream);
+}
+
+int ts_chunk_attn_kv8(const ts_chunk_shape *s, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                      const void *kv_scales, const int32_t *page_table, const int32_t *ctx_lens,
+                      const int32_t *q_starts, void *out, int64_t out_stride, float scale, void *workspace,
+                      size_t workspace_bytes, void *stream) {
+    return launch_chunk<true>(s, q, q_stride, k_pages, v_pages, kv_scales, page_table, ctx_lens, q_starts, out,
+                              out_stride, scale, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -81,6 +81,45 @@ def test_decode_binding_refuses_other_tensors():
         b.decode_attn_kv8(**good)
 
 
+def chunk(s, q=16, stride=512, k=16, v=16, scales=16, table=16, ctx=16, starts=16, out=16, out_stride=512, scale=0.125,
+          ws=256, nbytes=1 << 40):
+    return b.lib.ts_chunk_attn_kv8(ctypes.byref(s) if s else None, q, stride, k, v, scales, table, ctx, starts, out,
+                                   out_stride, ctypes.c_float(scale), ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", BAD_SHAPES, ids=str)
+def test_chunk_bad_shapes_rejected(kw):
+    s = shape(**kw)
+    assert b.lib.ts_chunk_attn_kv8_workspace_size(ctypes.byref(s)) == 0 and chunk(s) == -2
+
+
+def test_chunk_arguments_rejected():
+    s = shape()
+    need = b.chunk_kv8_workspace_size(s)
+    assert chunk(None) == -1
+    for name in ("q", "k", "v", "scales", "table", "ctx", "starts", "out", "ws"):
+        assert chunk(s, **{name: None}) == -1, name
+    assert chunk(s, nbytes=need - 1) == -3
+    for kw in (dict(ws=128), dict(q=8), dict(k=24), dict(v=2), dict(scales=4), dict(out=8), dict(stride=504),
+               dict(out_stride=0), dict(scale=float("inf")), dict(out=16, q=16, out_stride=520)):
+        assert chunk(s, **kw) == -6, kw
+    assert chunk(shape(num_tokens=0, max_q_len=0), q=None, scales=None) == 0
+
+
+def test_chunk_binding_refuses_other_tensors():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    pages, rows = torch.zeros(5, 2, 16, 64).to(torch.float8_e4m3fn), torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    good = dict(q=rows, k_pages=pages, v_pages=pages, kv_scales=torch.zeros(5, 2, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu),
+                page_table=i32(1, 2), ctx_lens=i32(1), q_starts=i32(2), out=rows.clone(), scale=1.0)
+    for name, bad in (("q ", rows.float()), ("k_pages", pages.bfloat16()), ("v_pages", pages[:4]),
+                      ("kv_scales", good["kv_scales"].view(torch.uint8)), ("page_table", i32(2)), ("ctx_lens", i32(2)),
+                      ("q_starts", i32(3)), ("out", rows[:2])):
+        with pytest.raises(ValueError, match=name):
+            b.chunk_attn_kv8(**{**good, name.strip(): bad})
+    with pytest.raises(ValueError, match="CUDA"):
+        b.chunk_attn_kv8(**good)
+
+
 def test_binding_refuses_other_types():
     bf, e4, e8 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
