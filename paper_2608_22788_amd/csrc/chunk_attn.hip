@@ -75,10 +75,10 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kRowBlock = 32;      // rows of a matrix-core tile
 constexpr int kChunkWaves = 8;
 // KV tiles in LDS: one in use, the others on their way.  Of the cache held in 8
-// bits: as bf16, one whose values are in use, one whose keys are, one being
-// converted; and as codes, on their way.  Both take 128 KiB at head_dim 128.
-constexpr int stages(bool k8) { return k8 ? 3 : 4; }
-constexpr int kCodeStages = 2;
+// bits: as bf16, the values in use with the keys of the next tile, and the place of
+// those after them; and as codes, on their way.  Both take 128 KiB at head_dim 128.
+constexpr int stages(bool k8) { return k8 ? 2 : 4; }
+constexpr int kCodeStages = 4;
 static_assert(kTileRows == kChunkWaves * kRowBlock, "a row block per wavefront");
 constexpr float kTiny = 1.17549435e-38f;   // the smallest normal float32
 constexpr float kLowest = -3.0e38f;       // the reference of a row without a score yet
@@ -308,8 +308,10 @@ __device__ __forceinline__ void dma_blocks(block_rsrc_t rsrc, uint32_t to, int f
 // Waits until at most the loads of the last `later` tiles are under way.
 template <int kLoads>
 __device__ __forceinline__ void dma_wait(int later) {
-    static_assert(stages(false) == 4 && kCodeStages == 2, "up to two later tiles");
-    if (later >= 2)
+    static_assert(stages(false) == 4 && kCodeStages == 4, "up to three later tiles");
+    if (later >= 3)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kLoads) : "memory");
+    else if (later == 2)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
     else if (later == 1)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
@@ -349,6 +351,7 @@ struct Chunk {
         // this lane's LDS addresses in stage 0, of the first keys and values
         uint32_t k, v;
         int from, twist;          // and where in a page it loads from (dma_blocks)
+        uint32_t to;              // where it stores the first of its codes as bf16, in stage 0
     };
 
     // The power of a wavefront's page, read as a scalar: the aligned word that holds
@@ -356,6 +359,13 @@ struct Chunk {
     struct Power {
         uint32_t word;
         int shift;
+        __device__ __forceinline__ static Power of(const ChunkParams &p, int pid, int g, int wave) {
+            if (pid < 0 || pid >= p.num_pages)
+                return {0x7f7f7f7fu, 0};   // (of zeros)
+            const size_t block = (size_t)pid * p.Hkv + g;
+            return {(uint32_t)ld_meta(reinterpret_cast<const int32_t *>(p.kv_scales), block / 2),
+                    16 * (int)(block % 2) + (wave < kTilePages ? 0 : 8)};
+        }
         __device__ __forceinline__ float value() const { return power_of(word >> shift & 0xff); }
     };
 
@@ -363,49 +373,41 @@ struct Chunk {
     // or values of a page, to `stage`.  A page outside the pool is stored as zeros;
     // what is under way then arrives first, so that counts of loads stay counts of
     // tiles.
-    __device__ __forceinline__ static Power dma_page(const ChunkParams &p, const State &st, int pid, bool once, int g, char *stage, int wave, int lane) {
+    __device__ __forceinline__ static void dma_page(const ChunkParams &p, const State &st, int pid, bool once, int g, char *stage, int wave, int lane) {
         char *to = stage + wave * kPageBytes;   // (the values follow the keys)
-        Power power = {0x7f7f7f7fu, 0};
         if (__builtin_expect(pid < 0 || pid >= p.num_pages, 0)) {
             dma_wait<kLoads>(0);
 #pragma unroll
             for (int i = 0; i < kLoads; i++)
                 *reinterpret_cast<u32x4_t *>(to + 16 * (i * kWave + lane)) = u32x4_t{0u, 0u, 0u, 0u};
-            return power;
+            return;
         }
         const size_t block = (size_t)pid * p.Hkv + g;
         const char *pages = reinterpret_cast<const char *>(wave < kTilePages ? p.k_pages : p.v_pages);
-        if constexpr (k8) {
-            power.word = (uint32_t)ld_meta(reinterpret_cast<const int32_t *>(p.kv_scales), block / 2);
-            power.shift = 16 * (int)(block % 2) + (wave < kTilePages ? 0 : 8);
-        }
         const block_rsrc_t rsrc = block_rsrc(pages + block * kPageBytes, kPageBytes);
         const uint32_t at = (uint32_t)first_lane_int((int)(uintptr_t)(lds_char *)to);
         if (once)
             dma_blocks<kLoads, true>(rsrc, at, st.from, st.twist);
         else
             dma_blocks<kLoads, false>(rsrc, at, st.from, st.twist);
-        return power;
     }
 
     // A wavefront's page of a tile from codes to bf16, times its power (exact), in the
     // order in which rows are stored: a lane takes back the 16 codes that it loaded,
-    // two pieces of a row.  NaN codes of values in `rows` rows (kClean) are replaced by
-    // zero; returns whether one of the first `rows` rows held one (clean_page).
-    __device__ __forceinline__ static bool convert_page(char *lds, int codes, int stage, float power, bool clean, int rows, int wave, int lane) {
+    // two pieces of a row.  With `clean`, NaN codes are replaced by zero; returns
+    // whether one of the first `rows` rows held one (the others are not in the
+    // context).
+    __device__ __forceinline__ static bool convert_page(const State &st, const char *codes, int stage, float power, bool clean, int rows, int wave,
+                                                        int lane) {
         constexpr int kLanes = D / 16;   // lanes of a row
-        const char *from = lds + kCodes + codes * kCodeBytes + wave * kPageBytes + 16 * lane;
-        char *to = lds + stage * kStage + wave * (kPage * kRowBytes);
-        const int piece = 2 * (lane % kLanes);
         bool any = false;
         u32x4_t c[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; i++)
-            c[i] = *reinterpret_cast<const u32x4_t *>(from + 1024 * i);
+            c[i] = *reinterpret_cast<const u32x4_t *>(codes + 16 * lane + 1024 * i);
+        if (__builtin_expect(clean, 0)) {
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const int row = i * (kWave / kLanes) + lane / kLanes;
-            if (__builtin_expect(clean, 0)) {
+            for (int i = 0; i < kLoads; i++) {
                 uint32_t odd = 0;
 #pragma unroll
                 for (int w = 0; w < 4; w++) {
@@ -413,8 +415,13 @@ struct Chunk {
                     c[i][w] &= ~((m >> 7) * 0xffu);
                     odd |= m;
                 }
-                any |= odd && row < rows;
+                any |= odd && i * (kWave / kLanes) + lane / kLanes < rows;
             }
+        }
+        // Block i holds rows 8 i .. of head_dim 128, whose key pieces differ by 8 i.
+        const uint32_t twist = wave < kTilePages ? 128 : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 u32x4_t x;
@@ -422,10 +429,9 @@ struct Chunk {
                 for (int w = 0; w < 4; w++)
                     x[w] = __builtin_bit_cast(uint32_t, w % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i][2 * u + w / 2], power, true)
                                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i][2 * u + w / 2], power, false));
-                const int at = wave < kTilePages ? k_piece(row, piece + u) : v_piece(row, piece + u);
-                *reinterpret_cast<u32x4_t *>(to + row * kRowBytes + 16 * at) = x;
+                lds_char *at = (lds_char *)(uintptr_t)((st.to ^ (16 * u + twist * i)) + stage * kStage);
+                *(lds_u32x4 *)(at + i * (kWave / kLanes) * kRowBytes) = x;
             }
-        }
         return any;
     }
 
@@ -447,6 +453,9 @@ struct Chunk {
         const bool keys = wave < kTilePages;
         st.from = k8 ? 16 * lane : row * kRowBytes + 16 * (keys ? k_piece(row, piece) : v_piece(row, piece));
         st.twist = keys && !k8 ? 64 : 0;
+        const int code_row = lane / (D / 16), code_piece = 2 * (lane % (D / 16));
+        st.to = base + (wave * kPage + code_row) * kRowBytes +
+                16 * (keys ? k_piece(code_row, code_piece) : v_piece(code_row, code_piece));
     }
 
     // Keys 32 kt .. + 31, dimensions 16 ks .. + 15.
@@ -673,7 +682,11 @@ struct Chunk {
         int first, last;   // page of the first tile; the last page of the context
         bool once;         // no other row tile reads them
         int ids[4];
-        Power power[kCodeStages];   // of the tiles on their way
+        // Codes: the power of the next tile to be converted, the id of its successor
+        // and the id of the next tile to be loaded, each read a tile ahead.
+        Power power;
+        int power_id, load_id;
+        __device__ __forceinline__ int id(int i) const { return ld_meta(pt, min(first + i * kTilePages, last)); }
         __device__ __forceinline__ int next(int i) {   // tiles i = 0, 1, ... of the piece, in order
             if (i % 4 == 0)
 #pragma unroll
@@ -688,12 +701,18 @@ struct Chunk {
     __device__ __forceinline__ static Pages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
         const SeqInfo sq = seq_info(p, pc.b);
         Pages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
-                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}, {}};
+                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}, {}, 0, 0};
         if constexpr (k8) {
 #pragma unroll
             for (int i = 0; i < kCodeStages; i++)
+                pages.ids[i] = pages.id(i);
+            pages.power = Power::of(p, first_lane_int(pages.ids[0]), pc.g, wave);
+            pages.power_id = first_lane_int(pages.ids[1]);
+            pages.load_id = pages.id(kCodeStages);
+#pragma unroll
+            for (int i = 0; i < kCodeStages; i++)
                 if (i < pc.j1 - pc.j0)
-                    pages.power[i] = dma_page(p, st, pages.next(i), pages.once, pc.g, lds + kCodes + i * kCodeBytes, wave, lane);
+                    dma_page(p, st, first_lane_int(pages.ids[i]), pages.once, pc.g, lds + kCodes + i * kCodeBytes, wave, lane);
         } else {
             const int n = min(pc.j1 - pc.j0, kStages - 1);
             for (int i = 0; i < n; i++)
@@ -762,37 +781,53 @@ struct Chunk {
                 lds_barrier();
             };
             // Codes: tile i becomes bf16 once it is there, and its place is loaded
-            // with tile i + 2.  A wavefront reads only codes that it loaded.
-            const auto convert = [&](int i, int slot) __attribute__((always_inline)) {
-                dma_wait<kLoads>(i + 1 < n ? 1 : 0);
-                const bool clean = i >= n_plain && wave >= kTilePages;
-                odd |= convert_page(lds, slot, i % kStages, pages.power[slot].value(), clean,
+            // with tile i + 4.  A wavefront reads only codes that it loaded.
+            const auto convert = [&](int i) __attribute__((always_inline)) {
+                if (i >= n)
+                    return;
+                dma_wait<kLoads>(min(n - 1 - i, kCodeStages - 1));
+                char *codes = lds + kCodes + i % kCodeStages * kCodeBytes;
+                odd |= convert_page(st, codes + wave * kPageBytes, i % kStages, pages.power.value(), i >= n_plain && wave >= kTilePages,
                                     sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage, wave, lane);
-                if (i + kCodeStages < n)
-                    pages.power[slot] = dma_page(p, st, pages.next(i + kCodeStages), pages.once, pc.g,
-                                                 lds + kCodes + slot * kCodeBytes, wave, lane);
+                pages.power = Power::of(p, pages.power_id, pc.g, wave);
+                pages.power_id = pages.id(i + 2);
+                if (i + kCodeStages < n) {
+                    dma_page(p, st, pages.load_id, pages.once, pc.g, codes, wave, lane);
+                    pages.load_id = pages.id(i + kCodeStages + 1);
+                }
+            };
+            // Step i reads the keys of tile i + 1 and the values of tile i.  Meanwhile the
+            // keys' wavefronts convert tile i + 2, before their own part of the step, and
+            // the values' tile i + 1, after it: a SIMD has one of each, so its matrix
+            // unit is not left alone.
+            const auto before = [&](int i) __attribute__((always_inline)) {
+                if (wave < kTilePages)
+                    convert(i + 2);
+            };
+            const auto after = [&](int i) __attribute__((always_inline)) {
+                if (wave >= kTilePages)
+                    convert(i + 1);
+                lds_barrier();
             };
             const auto room = [&](int i) { return st.lim - (pc.j0 + i) * kKeyTile - 4 * h; };
-            // (i % 2 == slot)
-            const auto advance = [&](int i, int slot) __attribute__((always_inline)) {
+            const auto advance = [&](int i) __attribute__((always_inline)) {
                 if constexpr (k8) {
-                    lds_barrier();
-                    if (i + 2 < n)
-                        convert(i + 2, slot);
+                    before(i);
                     return;
                 }
                 arrive(i + 1, min(n - 2 - i, 1));
                 if (i + kStages - 1 < n)
                     dma_page(p, st, pages.next(i + kStages - 1), pages.once, pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
-            const auto step = [&](int i, int slot, Scores &c, Scores &next) __attribute__((always_inline)) {
-                advance(i, slot);
+            const auto step = [&](int i, Scores &c, Scores &next) __attribute__((always_inline)) {
+                advance(i);
                 tile_step<true>(p, st, c, next, i % kStages * kStage, (i + 1) % kStages * kStage, i >= n_plain, room(i));
+                if constexpr (k8)
+                    after(i);
             };
             if constexpr (k8) {
-                convert(0, 0);
-                if (n > 1)
-                    convert(1, 1);
+                convert(0);
+                before(-1);
                 lds_barrier();
             } else {
                 arrive(0, min(n - 1, 2));
@@ -800,26 +835,32 @@ struct Chunk {
             if (__any(row_ok)) {
                 Scores a, b;
                 scores(st, 0, a);
+                if (k8 && n > 2)
+                    lds_barrier();   // step 0 replaces the first keys
                 largest(p, a);
                 for (int i = 0; i + 1 < n; i += 2) {
-                    step(i, 0, a, b);
+                    step(i, a, b);
                     if (i + 2 >= n) {
                         a = b;
                         break;
                     }
-                    step(i + 1, 1, b, a);
+                    step(i + 1, b, a);
                 }
                 tile_step<false>(p, st, a, b, (n - 1) % kStages * kStage, 0, n > n_plain, room(n - 1));
             } else {   // no row of this wavefront has a token: it only loads
-                for (int i = 0; i + 1 < n; i += 2) {
-                    advance(i, 0);
-                    if (i + 2 < n)
-                        advance(i + 1, 1);
+                if (k8 && n > 2)
+                    lds_barrier();
+                for (int i = 0; i + 1 < n; i++) {
+                    advance(i);
+                    if constexpr (k8)
+                        after(i);
                 }
             }
             lds_barrier();
             if (n_plain < n) {   // the same for every wavefront
-                int *flags = reinterpret_cast<int *>(lds + (kStages - 1) * kStage);   // the stage that start() leaves alone
+                // the stage that start() leaves alone (of codes, the values of the second
+                // tile, which are converted after a barrier)
+                int *flags = reinterpret_cast<int *>(lds + (kStages - 1) * kStage + (k8 ? kKBytes : 0));
                 const bool mine = __any(odd);
                 if (lane == 0)
                     flags[wave] = mine;
