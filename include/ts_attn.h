@@ -408,9 +408,7 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *                     aligned
  *   kv_scales         uint8 [num_pages][num_kv_heads][2], 16-byte aligned: the
  *                     biased exponents (e8m0) of a power of two for the keys and
- *                     one for the values of each page and KV head (where the last
- *                     pair ends in the middle of an aligned word of 4 bytes,
- *                     ts_chunk_attn_kv8 reads the whole word)
+ *                     one for the values of each page and KV head
  * A cached value is code * 2^(byte - 127), exactly a bf16 number for the bytes 27
  * to 227 that ts_rope_append_kv8 writes (the powers 2^-100 to 2^100); with others
  * the product is taken as bf16 takes it.  Code 0x7f (and 0xff) is NaN; e4m3 has no

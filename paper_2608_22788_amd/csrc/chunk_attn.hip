@@ -354,21 +354,6 @@ struct Chunk {
         uint32_t to;              // where it stores the first of its codes as bf16, in stage 0
     };
 
-    // The power of a wavefront's page, read as a scalar: the aligned word that holds
-    // its two bytes, and where in it this wavefront's is.
-    struct Power {
-        uint32_t word;
-        int shift;
-        __device__ __forceinline__ static Power of(const ChunkParams &p, int pid, int g, int wave) {
-            if (pid < 0 || pid >= p.num_pages)
-                return {0x7f7f7f7fu, 0};   // (of zeros)
-            const size_t block = (size_t)pid * p.Hkv + g;
-            return {(uint32_t)ld_meta(reinterpret_cast<const int32_t *>(p.kv_scales), block / 2),
-                    16 * (int)(block % 2) + (wave < kTilePages ? 0 : 8)};
-        }
-        __device__ __forceinline__ float value() const { return power_of(word >> shift & 0xff); }
-    };
-
     // Starts loading a wavefront's part of a tile, the keys (wavefronts 0 to 3)
     // or values of a page, to `stage`.  A page outside the pool is stored as zeros;
     // what is under way then arrives first, so that counts of loads stay counts of
@@ -682,11 +667,6 @@ struct Chunk {
         int first, last;   // page of the first tile; the last page of the context
         bool once;         // no other row tile reads them
         int ids[4];
-        // Codes: the power of the next tile to be converted, the id of its successor
-        // and the id of the next tile to be loaded, each read a tile ahead.
-        Power power;
-        int power_id, load_id;
-        __device__ __forceinline__ int id(int i) const { return ld_meta(pt, min(first + i * kTilePages, last)); }
         __device__ __forceinline__ int next(int i) {   // tiles i = 0, 1, ... of the piece, in order
             if (i % 4 == 0)
 #pragma unroll
@@ -696,23 +676,40 @@ struct Chunk {
             return first_lane_int(i & 2 ? hi : lo);
         }
     };
+    // Of codes, a lane holds one of 64 tiles: the id of the wavefront's page and the
+    // byte of its power, which reach their tile by lane reads.  (Scalar loads of them
+    // tile by tile would make every wait for LDS a wait for memory, since both are
+    // counted together: 16 ragged sequences 321 us.)
+    struct CodePages {
+        const int32_t *pt;
+        int first, last;   // as above
+        bool once;
+        int ids;           // of the 64 tiles of the next tile to be loaded
+        int bytes, later;  // of those of the next one to be converted, and of `ids`
+        __device__ __forceinline__ void fetch(const ChunkParams &p, int i, int g, int wave, int lane) {   // tiles i .. i + 63
+            const int pid = pt[min(first + (i + lane) * kTilePages, last)];
+            ids = pid;
+            later = 127;
+            if (pid >= 0 && pid < p.num_pages)
+                later = p.kv_scales[((size_t)pid * p.Hkv + g) * 2 + (wave < kTilePages ? 0 : 1)];
+        }
+        __device__ __forceinline__ int id(int i) const { return __builtin_amdgcn_readlane(ids, i % kWave); }
+        __device__ __forceinline__ float power(int i) const { return power_of(__builtin_amdgcn_readlane(bytes, i % kWave)); }
+    };
 
     // Starts loading the first tiles of a piece.
-    __device__ __forceinline__ static Pages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
+    typedef std::conditional_t<k8, CodePages, Pages> TilePages;
+    __device__ __forceinline__ static TilePages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
         const SeqInfo sq = seq_info(p, pc.b);
-        Pages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
-                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT, {}, {}, 0, 0};
+        TilePages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
+                    first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT};
         if constexpr (k8) {
-#pragma unroll
-            for (int i = 0; i < kCodeStages; i++)
-                pages.ids[i] = pages.id(i);
-            pages.power = Power::of(p, first_lane_int(pages.ids[0]), pc.g, wave);
-            pages.power_id = first_lane_int(pages.ids[1]);
-            pages.load_id = pages.id(kCodeStages);
+            pages.fetch(p, 0, pc.g, wave, lane);
+            pages.bytes = pages.later;
 #pragma unroll
             for (int i = 0; i < kCodeStages; i++)
                 if (i < pc.j1 - pc.j0)
-                    dma_page(p, st, first_lane_int(pages.ids[i]), pages.once, pc.g, lds + kCodes + i * kCodeBytes, wave, lane);
+                    dma_page(p, st, pages.id(i), pages.once, pc.g, lds + kCodes + i * kCodeBytes, wave, lane);
         } else {
             const int n = min(pc.j1 - pc.j0, kStages - 1);
             for (int i = 0; i < n; i++)
@@ -745,7 +742,7 @@ struct Chunk {
         bool first = pc.us <= begin;   // the range starts inside it: its partial result's slot
         State st;
         set_addresses(st, lds, wave, lane);
-        Pages pages = start(p, st, pc, lds, wave, lane);
+        TilePages pages = start(p, st, pc, lds, wave, lane);
         for (;;) {
             const SeqInfo sq = seq_info(p, pc.b);
             const int token = pc.m * p.TT + r / p.G;
@@ -783,17 +780,21 @@ struct Chunk {
             // Codes: tile i becomes bf16 once it is there, and its place is loaded
             // with tile i + 4.  A wavefront reads only codes that it loaded.
             const auto convert = [&](int i) __attribute__((always_inline)) {
-                if (i >= n)
-                    return;
-                dma_wait<kLoads>(min(n - 1 - i, kCodeStages - 1));
-                char *codes = lds + kCodes + i % kCodeStages * kCodeBytes;
-                odd |= convert_page(st, codes + wave * kPageBytes, i % kStages, pages.power.value(), i >= n_plain && wave >= kTilePages,
-                                    sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage, wave, lane);
-                pages.power = Power::of(p, pages.power_id, pc.g, wave);
-                pages.power_id = pages.id(i + 2);
-                if (i + kCodeStages < n) {
-                    dma_page(p, st, pages.load_id, pages.once, pc.g, codes, wave, lane);
-                    pages.load_id = pages.id(i + kCodeStages + 1);
+                if constexpr (k8) {
+                    if (i >= n)
+                        return;
+                    dma_wait<kLoads>(min(n - 1 - i, kCodeStages - 1));
+                    char *codes = lds + kCodes + i % kCodeStages * kCodeBytes;
+                    if (__builtin_expect(i % kWave == 0 && i > 0, 0))
+                        pages.bytes = pages.later;
+                    odd |= convert_page(st, codes + wave * kPageBytes, i % kStages, pages.power(i), i >= n_plain && wave >= kTilePages,
+                                        sq.L - ((pc.j0 + i) * kTilePages + wave % kTilePages) * kPage, wave, lane);
+                    const int next = i + kCodeStages;
+                    if (next < n) {
+                        if (__builtin_expect(next % kWave == 0, 0))
+                            pages.fetch(p, next, pc.g, wave, lane);
+                        dma_page(p, st, pages.id(next), pages.once, pc.g, codes, wave, lane);
+                    }
                 }
             };
             // Step i reads the keys of tile i + 1 and the values of tile i.  Meanwhile the
@@ -813,11 +814,11 @@ struct Chunk {
             const auto advance = [&](int i) __attribute__((always_inline)) {
                 if constexpr (k8) {
                     before(i);
-                    return;
+                } else {
+                    arrive(i + 1, min(n - 2 - i, 1));
+                    if (i + kStages - 1 < n)
+                        dma_page(p, st, pages.next(i + kStages - 1), pages.once, pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
                 }
-                arrive(i + 1, min(n - 2 - i, 1));
-                if (i + kStages - 1 < n)
-                    dma_page(p, st, pages.next(i + kStages - 1), pages.once, pc.g, lds + (i + kStages - 1) % kStages * kStage, wave, lane);
             };
             const auto step = [&](int i, Scores &c, Scores &next) __attribute__((always_inline)) {
                 advance(i);
