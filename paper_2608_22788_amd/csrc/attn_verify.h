@@ -111,7 +111,12 @@ struct Verify {
     }
     __device__ static void load_block(const AttnParams &p, int pid, bool in, int g, int n, int kq, int h, Kv8Regs &r) {
         const size_t block = (size_t)pid * p.Hkv + g;
-        r.power[h] = reinterpret_cast<const uint16_t *>(p.kv_scales)[block];
+        // Every lane loads the same two bytes, at an offset that the compiler does not
+        // know to be the same: a uniform load would be made a scalar, which has to be
+        // waited for here, in front of the pages of this step (bulk decode 374 us).
+        uint32_t none;
+        asm("v_mov_b32 %0, 0" : "=v"(none));
+        r.power[h] = *reinterpret_cast<const uint16_t *>(p.kv_scales + 2 * block + none);
         const block_rsrc_t rk = block_rsrc(reinterpret_cast<const uint8_t *>(p.k_pages) + block * (kPage * D), in ? kBlockBytes : 0);
         const block_rsrc_t rv = block_rsrc(reinterpret_cast<const uint8_t *>(p.v_pages) + block * (kPage * D), in ? kBlockBytes : 0);
 #pragma unroll
