@@ -500,7 +500,7 @@ typedef struct ts_rules_config {
     int32_t vocab;
     int32_t logits_type;        /* TS_LOGITS_F32 or TS_LOGITS_BF16 */
     int32_t out_type;
-    int32_t max_tokens;         /* up to 2^30; used with tokens */
+    int32_t max_tokens;         /* up to 2^29; used with tokens */
     int32_t num_biases;         /* up to 2^30; used with biases */
     int64_t row_stride, out_stride;   /* elements */
     int64_t token_stride;       /* elements, at least max_tokens */

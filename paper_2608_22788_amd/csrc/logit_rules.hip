@@ -19,8 +19,15 @@
 //
 // In place, a thread that has nothing to change neither reads nor writes.
 //
-// What bounds it: memory where there are many rows (logits in and out, the mask,
-// the tokens); the chain lengths -> tokens -> LDS -> stores where there are few.
+// What bounds it.  Many rows: vector instructions, busy 85 % of the time at 200 rows
+// of 151,936 bf16 logits, masks, biases and texts of 4,000 tokens on average (45 us;
+// the bytes alone need 26): 133 for a wavefront's 512 tokens of the vocabulary and
+// about as many for the text, the biases and addresses.  Slices of 8,192 tokens on
+// 1,024 threads take 47 us, on 512 threads 47, 4,096 on 256 threads 50.  Workgroups
+// that keep a row's text for several slices gain nothing (49), and working out only
+// the tokens of the text, whoever finds their count, is a longer chain (77).  Few
+// rows: the chain lengths -> tokens -> LDS -> stores (8 rows 7 us, less than the call
+// from Python).
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"
@@ -31,10 +38,11 @@ namespace tsattn {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kPer = 8;                        // tokens of a thread
 constexpr int kSlice = kThreads * kPer;
 constexpr int kAhead = 4;                      // groups of four text tokens whose loads are in flight together
+constexpr int kTable = kSlice + kWave;          // and a place for each lane's tokens of other slices
 constexpr uint32_t kInPrompt = 0x80000000u;
 
 struct RulesParams {
@@ -110,7 +118,7 @@ __device__ __forceinline__ void lds_sync() {
 
 // A penalty, or `off` where it is not given or not finite.
 __device__ __forceinline__ float penalty(const float *p, int b, float off) {
-    const float x = p ? p[b] : off;
+    const float x = p ? __int_as_float(ld_meta(reinterpret_cast<const int32_t *>(p), b)) : off;
     return fabsf(x) < INFINITY ? x : off;
 }
 
@@ -118,103 +126,145 @@ template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
     uint32_t *const count = lds;                              // [kSlice] times in the answer; kInPrompt
-    float *const bias = reinterpret_cast<float *>(lds + kSlice);   // [kSlice], where there are biases
+    float *const bias = reinterpret_cast<float *>(lds + kTable);   // [kSlice], where there are biases
     __shared__ int s_pending;
     const int at = xcd_worker(blockIdx.x, gridDim.x);
     const int b = at / p.slices, base = at % p.slices * kSlice, tid = threadIdx.x;
     const int n = p.vocab - base - kPer * tid;                // of this thread's tokens exist
     const TI *const src = static_cast<const TI *>(p.logits) + b * p.row_stride + base + kPer * tid;
     TO *const dst = static_cast<TO *>(p.out) + b * p.out_stride + base + kPer * tid;
+    const uint32_t here = (uint32_t)min(kSlice, p.vocab - base);   // tokens of the slice
+    // Lengths, then every first load, before anything waits for one.
+    int first = 0, end = 0, len = 0, prompt = 0;
+    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
+    if (p.bias_tokens) {
+        first = ld_meta(p.bias_starts, b);
+        end = ld_meta(p.bias_starts, b + 1);
+    }
+    if (p.tokens) {
+        len = ld_meta(p.lens, b);
+        prompt = p.prompt_lens ? ld_meta(p.prompt_lens, b) : 0;
+        rep = penalty(p.repetition, b, 1.0f);
+        rep = rep > 0.0f ? rep : 1.0f;
+        freq = penalty(p.frequency, b, 0.0f);
+        pres = penalty(p.presence, b, 0.0f);
+    }
     float x[kPer];
     if (!p.in_place)
         load8(src, n, x);
     uint32_t closed = 0;                                      // bit e: token e is not allowed
     if (p.allowed && n > 0) {
         const int v = base + kPer * tid;
-        closed = ~p.allowed[b * p.allowed_stride + v / 32] >> v % 32 & 0xff;
+        closed = ~p.allowed[b * p.allowed_stride + v / 32] >> v % 32 & ((1u << kPer) - 1);
     }
+    first = min(max(first, 0), p.num_biases);
+    end = min(max(end, 0), p.num_biases);
+    len = min(max(len, 0), p.max_tokens);
+    prompt = min(max(prompt, 0), len);
+    uint32_t bias_at = ~0u;                                   // place in the slice of the bias that this thread holds
+    float bias_w = 0.0f;
+    const auto load_bias = [&](int j0) {
+        const int j = j0 + tid;
+        bias_at = j < end ? (uint32_t)p.bias_tokens[j] - (uint32_t)base : ~0u;
+        bias_w = j < end ? p.bias_values[j] : 0.0f;
+    };
+    if (first < end)
+        load_bias(first);
+    const int32_t *const text = p.tokens + (p.tokens ? b * p.token_stride : 0);
+    const int whole = len / 4 * 4;
+    Many<int32_t, 4> ids[kAhead];
+    // Groups of four tokens from i0 on, -1 where the text has none (the conditions on
+    // whole wavefronts are scalar).
+    const int lane4 = 4 * (tid % kWave), wave4 = first_lane_int(4 * (tid - tid % kWave));
+    const auto load_text = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) {
+            const int at = i0 + wave4 + 4 * kThreads * k;
+            ids[k] = Many<int32_t, 4>{{-1, -1, -1, -1}};
+            if (at < whole && at + lane4 < whole)
+                ids[k] = *reinterpret_cast<const Many<int32_t, 4> *>(text + at + lane4);
+        }
+    };
+    load_text(0);
+    const int32_t odd = whole + tid < len ? text[whole + tid] : -1;   // the last tokens
+
     u32x4_t *const zero = reinterpret_cast<u32x4_t *>(lds);
 #pragma unroll
     for (int i = 0; i < kSlice / 4 / kThreads; i++) {
         zero[i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
         if (p.bias_tokens)
-            zero[kSlice / 4 + i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
+            zero[kTable / 4 + i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
     }
     lds_sync();
 
-    if (p.bias_tokens) {
-        const int first = min(max(ld_meta(p.bias_starts, b), 0), p.num_biases);
-        const int end = min(max(ld_meta(p.bias_starts, b + 1), 0), p.num_biases);
-        for (int j0 = first; j0 < end; j0 += kThreads) {
-            const int j = j0 + tid;
-            const uint32_t t = j < end ? (uint32_t)p.bias_tokens[j] - (uint32_t)base : ~0u;
-            bool pending = t < (uint32_t)min(kSlice, p.vocab - base);
-            const float w = pending ? p.bias_values[j] : 0.0f;
-            const uint32_t mine = kThreads - tid;             // the first thread has the largest
-            for (;;) {
-                if (tid == 0)
-                    s_pending = 0;
-                if (pending)
-                    atomicMax(&count[t], mine);
-                lds_sync();
-                const bool turn = pending && count[t] == mine;
-                if (pending && !turn)
-                    s_pending = 1;
-                lds_sync();
-                if (turn) {
-                    bias[t] += w;
-                    count[t] = 0;
-                    pending = false;
-                }
-                const int more = s_pending;
-                lds_sync();
-                if (!more)
-                    break;
+    for (int j0 = first; j0 < end; j0 += kThreads) {
+        bool pending = bias_at < here;
+        const uint32_t mine = kThreads - tid;             // the first thread has the largest
+        for (;;) {
+            if (tid == 0)
+                s_pending = 0;
+            if (pending)
+                atomicMax(&count[bias_at], mine);
+            lds_sync();
+            const bool turn = pending && count[bias_at] == mine;
+            if (pending && !turn)
+                s_pending = 1;
+            lds_sync();
+            if (turn) {
+                bias[bias_at] += bias_w;
+                count[bias_at] = 0;
+                pending = false;
             }
+            const int more = s_pending;
+            lds_sync();
+            if (!more)
+                break;
         }
+        if (j0 + kThreads < end)
+            load_bias(j0 + kThreads);
     }
 
-    float rep = 1.0f, freq = 0.0f, pres = 0.0f;
     if (p.tokens) {
-        const int len = min(max(ld_meta(p.lens, b), 0), p.max_tokens);
-        const int prompt = p.prompt_lens ? min(max(ld_meta(p.prompt_lens, b), 0), len) : 0;
-        const int32_t *const text = p.tokens + b * p.token_stride;
-        const uint32_t here = (uint32_t)min(kSlice, p.vocab - base);
-        const auto add = [&](int i, int32_t token) {
+        // No branches: a token of another slice goes to a place of the lane's own.
+        const uint32_t aside = kSlice + tid % kWave;
+        const auto place = [&](int32_t token, bool counts) {
             const uint32_t t = (uint32_t)token - (uint32_t)base;
-            if (t < here) {
-                if (i < prompt)
-                    atomicOr(&count[t], kInPrompt);
-                else
-                    atomicAdd(&count[t], 1u);
-            }
+            return counts && t < here ? t : aside;
         };
-        const int whole = len / 4 * 4;
-        for (int i0 = 4 * tid; i0 < whole; i0 += 4 * kThreads * kAhead) {
-            Many<int32_t, 4> v[kAhead];
+        for (int i0 = 0; i0 < whole; i0 += 4 * kThreads * kAhead) {
+            if (i0 > 0)
+                load_text(i0);
 #pragma unroll
-            for (int k = 0; k < kAhead; k++)
-                v[k] = *reinterpret_cast<const Many<int32_t, 4> *>(text + (i0 + 4 * kThreads * k < whole ? i0 + 4 * kThreads * k : i0));
-#pragma unroll
-            for (int k = 0; k < kAhead; k++)
-                if (i0 + 4 * kThreads * k < whole)
+            for (int k = 0; k < kAhead; k++) {
+                const int at = i0 + wave4 + 4 * kThreads * k;
+                if (at >= whole)
+                    break;
+                if (at >= prompt) {
 #pragma unroll
                     for (int e = 0; e < 4; e++)
-                        add(i0 + 4 * kThreads * k + e, v[k].x[e]);
+                        atomicAdd(&count[place(ids[k].x[e], true)], 1u);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        atomicOr(&count[place(ids[k].x[e], at + lane4 + e < prompt)], kInPrompt);
+                    if (at + 4 * kWave > prompt)
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            atomicAdd(&count[place(ids[k].x[e], at + lane4 + e >= prompt)], 1u);
+                }
+            }
         }
-        if (whole + tid < len)
-            add(whole + tid, text[whole + tid]);
-        rep = penalty(p.repetition, b, 1.0f);
-        rep = rep > 0.0f ? rep : 1.0f;
-        freq = penalty(p.frequency, b, 0.0f);
-        pres = penalty(p.presence, b, 0.0f);
+        if (tid < 4) {
+            atomicOr(&count[place(odd, whole + tid < prompt)], kInPrompt);
+            atomicAdd(&count[place(odd, whole + tid >= prompt)], 1u);
+        }
         lds_sync();
     }
     if (n <= 0)
         return;
     uint32_t c[kPer];
     float w[kPer];
-    uint32_t any = closed;
+    bool any = closed != 0;
 #pragma unroll
     for (int e = 0; e < kPer; e += 4) {
         const u32x4_t cv = *reinterpret_cast<const u32x4_t *>(count + kPer * tid + e);
@@ -225,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
         for (int i = 0; i < 4; i++) {
             c[e + i] = cv[i];
             w[e + i] = wv[i];
-            any |= cv[i] | (wv[i] != 0.0f);   // (NaN differs from 0)
+            any |= cv[i] != 0 || wv[i] != 0.0f;   // (NaN differs from 0)
         }
     }
     if (p.in_place) {
@@ -233,13 +283,13 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
             return;
         load8(src, n, x);
     }
+    // (Without branches, which some token of a wavefront's 512 would mostly take.)
+    const float inverse = 1.0f / rep;
 #pragma unroll
     for (int e = 0; e < kPer; e++) {
-        if (c[e]) {
-            const uint32_t times = c[e] & ~kInPrompt;
-            x[e] = x[e] > 0.0f ? x[e] / rep : x[e] * rep;
-            x[e] -= times ? freq * (float)times + pres : 0.0f;
-        }
+        const uint32_t times = c[e] & ~kInPrompt;
+        x[e] *= c[e] ? x[e] > 0.0f ? inverse : rep : 1.0f;
+        x[e] -= times ? freq * (float)times + pres : 0.0f;
         x[e] += w[e];
         x[e] = closed >> e & 1 ? -INFINITY : x[e];
     }
@@ -324,7 +374,7 @@ int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, co
     const auto kernel = f_in ? f_out ? logit_rules_kernel<float, float> : logit_rules_kernel<float, uint16_t>
                              : f_out ? logit_rules_kernel<uint16_t, float> : logit_rules_kernel<uint16_t, uint16_t>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(cfg->num_seqs * p.slices)), dim3(kThreads),
-                       kSlice * sizeof(uint32_t) * (p.bias_tokens ? 2 : 1), reinterpret_cast<hipStream_t>(stream), p);
+                       (kTable + (p.bias_tokens ? kSlice : 0)) * sizeof(uint32_t), reinterpret_cast<hipStream_t>(stream), p);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? TS_OK : hip_fail(e, "logit rules launch");
 }

@@ -31,7 +31,7 @@ def test_bad_shapes_rejected(kw):
 
 @pytest.mark.parametrize("kw", [
     dict(logits_type=2), dict(out_type=-1), dict(row_stride=99), dict(out_stride=99), dict(row_stride=1 << 41),
-    dict(max_tokens=-1), dict(max_tokens=(1 << 30) + 1), dict(token_stride=9), dict(num_biases=-1),
+    dict(max_tokens=-1), dict(max_tokens=(1 << 29) + 1), dict(token_stride=9), dict(num_biases=-1),
     dict(num_biases=(1 << 30) + 1), dict(allowed_stride=3)], ids=str)
 def test_bad_arguments_rejected(kw):
     assert rules(config(**kw)) == -6 and b.lib.ts_last_error()
