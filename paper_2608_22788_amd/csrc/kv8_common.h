@@ -38,6 +38,18 @@ __device__ __forceinline__ uint32_t pack_codes4(const float *x, float inv) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(code_value(x[0], inv), code_value(x[1], inv), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_value(x[2], inv), code_value(x[3], inv), w, true);
 }
+// Eight values over `power` as codes, nearest even, where none is larger than 448 times
+// it, infinite or NaN: the conversion divides by the power itself.
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2_t codes8(const float x[8], float power) {
+    s16x2_t w[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[i], x[4 * i], x[4 * i + 1], power, false);
+        w[i] = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w[i], x[4 * i + 2], x[4 * i + 3], power, true);
+    }
+    return u32x2_t{__builtin_bit_cast(uint32_t, w[0]), __builtin_bit_cast(uint32_t, w[1])};
+}
 // Four codes times `factor` as codes.
 __device__ __forceinline__ uint32_t scale_codes4(uint32_t w, float factor) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);

@@ -48,26 +48,43 @@ struct Rope8Params {
 
 constexpr int kQueries = 4;   // query heads whose loads are in flight together
 
-__device__ __forceinline__ float max_abs8(const float x[8]) {
-    float m = 0.0f;
+// The largest of eight sizes, as the bits of a float: those of infinite and NaN values
+// are above every finite one's.
+__device__ __forceinline__ uint32_t max_abs8(const float x[8]) {
+    uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; e++)
-        m = fmaxf(m, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.0f);
+        m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
     return m;
 }
-__device__ __forceinline__ float max_wave(float x) {
-    x = fmaxf(x, dpp_f32<kDppXor1>(x));
-    x = fmaxf(x, dpp_f32<kDppXor2>(x));
-    x = fmaxf(x, dpp_f32<kDppHalfMirror>(x));
-    x = fmaxf(x, dpp_f32<kDppMirror>(x));
-    return max_across_lane_groups(x);
+// Finite values alone.
+__device__ __forceinline__ uint32_t max_finite8(const float x[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const uint32_t u = __float_as_uint(x[e]) & 0x7fffffffu;
+        m = max(m, u < 0x7f800000u ? u : 0u);
+    }
+    return m;
+}
+// Of a wavefront.  (The bits of sizes compare as the sizes do, but for NaN.)
+__device__ __forceinline__ uint32_t max_wave(uint32_t x) {
+    const auto step = [&](int y) { x = max(x, (uint32_t)y); };
+    step(__builtin_amdgcn_update_dpp(0, (int)x, kDppXor1, 0xf, 0xf, true));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, kDppXor2, 0xf, 0xf, true));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, kDppHalfMirror, 0xf, 0xf, true));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, kDppMirror, 0xf, 0xf, true));
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(h[0], h[1]);
 }
 
 template <int D>
 __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Params p) {
     constexpr int kLanes = D / 8;                  // lanes per head
     constexpr int kWaves = kPage * kLanes / kWave;
-    __shared__ float s_max[2][kWaves];
+    __shared__ uint32_t s_max[2][kWaves], s_finite[2][kWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int slot = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
     const int g = blockIdx.y, T = p.num_tokens;
@@ -121,7 +138,7 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
     const bool upper = !p.interleaved && c >= pieces;
     const int other = p.interleaved ? c : c < pieces ? c + pieces : c < 2 * pieces ? c - pieces : c;
     const bool turns_here = 8 * c < p.rot;
-    float co[8], si[8];
+    float co[8], si[8];                            // interleaved: of pair e / 2
     const auto angles = [&]() __attribute__((always_inline)) {
         const int j = p.interleaved ? 4 * c : upper ? 8 * (c - pieces) + 4 : 8 * c;
         float mc[4], ms[4];
@@ -134,109 +151,136 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
                 sincospif((float)(2.0 * (turns - rint(turns))), &ms[e], &mc[e]);
             }
         }
+        if (p.interleaved) {
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const float pc = __shfl(mc[e], lane - c + other, kWave), ps = __shfl(ms[e], lane - c + other, kWave);
-            co[e] = upper ? pc : mc[e];
-            si[e] = upper ? ps : ms[e];
-            co[e + 4] = upper ? mc[e] : pc;
-            si[e + 4] = upper ? ms[e] : ps;
+            for (int e = 0; e < 8; e++) {
+                co[e] = mc[e / 2];
+                si[e] = e % 2 ? ms[e / 2] : -ms[e / 2];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float pc = __shfl(mc[e], lane - c + other, kWave), ps = __shfl(ms[e], lane - c + other, kWave);
+                co[e] = upper ? pc : mc[e];
+                si[e] = upper ? ps : -ms[e];
+                co[e + 4] = upper ? mc[e] : pc;
+                si[e + 4] = upper ? ms[e] : -ps;
+            }
         }
     };
-    // One head's values after its norm and rotation.
-    const auto turned = [&](u32x4_t raw, const uint16_t *w, float x[8]) __attribute__((always_inline)) {
+    // A head's value is r (x a + z b), z its partner in the pair and r its norm's
+    // factor, with the norm's weights in a and b.
+    const auto factors = [&](const uint16_t *w, float a[8], float b[8]) __attribute__((always_inline)) {
+        float wx[8], wz[8];
+        if (w) {
+            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * c), wx);
+            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * other), wz);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            a[e] = w ? wx[e] * co[e] : co[e];
+            b[e] = w ? (p.interleaved ? wx[e ^ 1] : wz[e]) * si[e] : si[e];
+        }
+    };
+    const auto turned = [&](u32x4_t raw, bool norm, const float a[8], const float b[8], float x[8]) __attribute__((always_inline)) {
         u32x4_t raw2;
 #pragma unroll
-        for (int e = 0; e < 4; e++)
-            raw2[e] = __shfl(raw[e], lane - c + other, kWave);
+        for (int e = 0; e < 4; e++) {
+            raw2[e] = p.interleaved ? raw[e] << 16 | raw[e] >> 16 : __shfl(raw[e], lane - c + other, kWave);
+            raw2[e] = turns_here ? raw2[e] : 0;    // (an infinite value times a sine of zero)
+        }
         float z[8];
         unpack8(raw, x);
         unpack8(raw2, z);
-        if (w) {
+        float r = 1.0f;
+        if (norm) {
             float ss = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; e++)
                 ss += x[e] * x[e];
-            const float r = 1.0f / sqrtf(sum_head<kLanes>(ss) * (1.0f / D) + p.eps);
-            float wx[8], wz[8];
-            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * c), wx);
-            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * other), wz);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                x[e] *= r * wx[e];
-                z[e] *= r * wz[e];
-            }
+            r = __builtin_amdgcn_rsqf(sum_head<kLanes>(ss) * (1.0f / D) + p.eps);
         }
-        if (turns_here) {
-            if (p.interleaved) {
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float a = x[2 * e], d = x[2 * e + 1];
-                    x[2 * e] = a * co[e] - d * si[e];
-                    x[2 * e + 1] = d * co[e] + a * si[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    x[e] = upper ? x[e] * co[e] + z[e] * si[e] : x[e] * co[e] - z[e] * si[e];
-            }
-        }
+        for (int e = 0; e < 8; e++)
+            x[e] = (x[e] * a[e] + z[e] * b[e]) * r;
     };
 
     const bool busy = __any(active);               // this wavefront has a row
-    float xk[8], xv[8];
-    unpack8(raw_v, xv);
+    float xk[8], a[8], f[8];
     if (busy) {
         angles();
-        turned(raw_k, p.k_norm, xk);
-        const float mk = max_wave(active ? max_abs8(xk) : 0.0f), mv = max_wave(max_abs8(xv));
+        factors(p.k_norm, a, f);
+        turned(raw_k, p.k_norm, a, f, xk);
+        float xv[8];
+        unpack8(raw_v, xv);
+        const uint32_t mk = max_wave(active ? max_abs8(xk) : 0), mv = max_wave(max_abs8(xv));
+        uint32_t fk = mk, fv = mv;
+        if (__builtin_expect(max(mk, mv) >= 0x7f800000u, 0)) {
+            fk = max_wave(active ? max_finite8(xk) : 0);
+            fv = max_wave(max_finite8(xv));
+        }
         if (lane == 0) {
             s_max[0][wave] = mk;
             s_max[1][wave] = mv;
+            s_finite[0][wave] = fk;
+            s_finite[1][wave] = fv;
         }
     } else if (lane == 0) {
-        s_max[0][wave] = s_max[1][wave] = 0.0f;
+        s_max[0][wave] = s_max[1][wave] = s_finite[0][wave] = s_finite[1][wave] = 0;
     }
     __syncthreads();   // (every thread has also read the held tokens' powers)
     if (block >= 0) {
-        float mk = s_max[0][0], mv = s_max[1][0];
+        uint32_t m = 0, mk = 0, mv = 0;            // infinite values and NaN among them; without
 #pragma unroll
-        for (int i = 1; i < kWaves; i++) {
-            mk = fmaxf(mk, s_max[0][i]);
-            mv = fmaxf(mv, s_max[1][i]);
+        for (int i = 0; i < kWaves; i++) {
+            m = max(m, max(s_max[0][i], s_max[1][i]));
+            mk = max(mk, s_finite[0][i]);
+            mv = max(mv, s_finite[1][i]);
         }
-        int kb = power_for(mk), vb = power_for(mv);
+        int kb = power_for(__uint_as_float(mk)), vb = power_for(__uint_as_float(mv));
         const int kh = old & 0xff, vh = old >> 8;
         if (held > 0) {
             kb = min(max(kb, kh), kHighestPower);
             vb = min(max(vb, vh), kHighestPower);
             if (slot < held) {
                 if (kb != kh) {
-                    const float f = power_of(kh) * power_of(254 - kb);
-                    *reinterpret_cast<u32x2_t *>(p.k_pages + code_at) = u32x2_t{scale_codes4(old_k[0], f), scale_codes4(old_k[1], f)};
+                    const float s = power_of(kh) * power_of(254 - kb);
+                    *reinterpret_cast<u32x2_t *>(p.k_pages + code_at) = u32x2_t{scale_codes4(old_k[0], s), scale_codes4(old_k[1], s)};
                 }
                 if (vb != vh) {
-                    const float f = power_of(vh) * power_of(254 - vb);
-                    *reinterpret_cast<u32x2_t *>(p.v_pages + code_at) = u32x2_t{scale_codes4(old_v[0], f), scale_codes4(old_v[1], f)};
+                    const float s = power_of(vh) * power_of(254 - vb);
+                    *reinterpret_cast<u32x2_t *>(p.v_pages + code_at) = u32x2_t{scale_codes4(old_v[0], s), scale_codes4(old_v[1], s)};
                 }
             }
         }
         if (active) {
-            const float ik = power_of(254 - kb), iv = power_of(254 - vb);
-            *reinterpret_cast<u32x2_t *>(p.k_pages + code_at) = u32x2_t{pack_codes4(xk, ik), pack_codes4(xk + 4, ik)};
-            *reinterpret_cast<u32x2_t *>(p.v_pages + code_at) = u32x2_t{pack_codes4(xv, iv), pack_codes4(xv + 4, iv)};
+            u32x2_t ck, cv;
+            float xv[8];
+            unpack8(raw_v, xv);
+            if (__builtin_expect(m <= __float_as_uint(kLargestCode * 0x1p100f), 1)) {   // all inside their power's range
+                ck = codes8(xk, power_of(kb));
+                cv = codes8(xv, power_of(vb));
+            } else {
+                const float ik = power_of(254 - kb), iv = power_of(254 - vb);
+                ck = u32x2_t{pack_codes4(xk, ik), pack_codes4(xk + 4, ik)};
+                cv = u32x2_t{pack_codes4(xv, iv), pack_codes4(xv + 4, iv)};
+            }
+            *reinterpret_cast<u32x2_t *>(p.k_pages + code_at) = ck;
+            *reinterpret_cast<u32x2_t *>(p.v_pages + code_at) = cv;
         }
         if (threadIdx.x == 0)
             *power = (uint16_t)(kb | vb << 8);
     }
     if (!busy)
         return;
+    if (p.q_norm || p.k_norm)
+        factors(p.q_norm, a, f);
     for (int h0 = 0;;) {
 #pragma unroll
         for (int i = 0; i < kQueries; i++) {
             if (h0 + i < p.G) {
                 float x[8];
-                turned(raw_q[i], p.q_norm, x);
+                turned(raw_q[i], p.q_norm, a, f, x);
                 if (active)
                     *reinterpret_cast<u32x4_t *>(p.q_out + row * p.q_out_stride + (int64_t)(g * p.G + h0 + i) * D + 8 * c) = pack8(x);
             }
