@@ -151,3 +151,46 @@ def test_oracle_codes_are_e4m3():
 def test_oracle_power(amax, byte):
     assert kv8.power_byte(amax) == byte
     assert amax <= 448.0 * 2.0 ** (byte - 127) or byte == 227
+
+
+def test_every_call_hands_its_stream_and_tensors_to_the_device_check(monkeypatch):
+    seen = []
+
+    def check(*tensors, stream=None):
+        seen.append((len(tensors), stream))
+        raise ValueError("stop")
+
+    monkeypatch.setattr(b, "_check_device", check)
+    bf = lambda *s: torch.ones(*s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.ones(*s, dtype=torch.int32)  # noqa: E731
+    pages = torch.zeros(3, 2, 16, 64).to(torch.float8_e4m3fn)
+    scales = torch.zeros(3, 2, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    cache = (pages, pages, scales, i32(2, 2), i32(2))
+    s = object()
+    for call, n in ((lambda: b.chunk_attn_kv8(bf(5, 4, 64), *cache, i32(3), bf(5, 4, 64), 1.0, stream=s), 9),
+                    (lambda: b.decode_attn_kv8(bf(2, 1, 4, 64), *cache, i32(2), bf(2, 1, 4, 64), 1.0, stream=s), 9),
+                    (lambda: b.rope_append_kv8(bf(5, 4, 64), bf(5, 2, 64), bf(5, 2, 64), bf(5, 4, 64), *cache, i32(3), None,
+                                               stream=s), 13),
+                    (lambda: b.logit_rules(torch.ones(2, 8), torch.ones(2, 8), stream=s), 12)):
+        with pytest.raises(ValueError, match="stop"):
+            call()
+        assert seen.pop() == (n, s)
+
+
+@pytest.mark.parametrize("call, kind", [("decode_attn_kv8", "zeros"), ("chunk_attn_kv8", "empty")])
+def test_own_workspaces_are_made_on_the_calls_stream(monkeypatch, call, kind):
+    made = []
+    monkeypatch.setattr(b, "_check_device", lambda *t, **kw: None)
+    monkeypatch.setattr(b, "_stream_ptr", lambda s: 7)
+    monkeypatch.setattr(b, "_own_workspace", lambda n, device, stream, zeros=False: made.append((stream, zeros)) or
+                        torch.zeros(n, dtype=torch.uint8))
+    monkeypatch.setattr(b, "check", lambda *a: None)
+    monkeypatch.setattr(b.lib, "ts_" + call, lambda *a: 0)
+    bf = lambda *s: torch.ones(*s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.ones(*s, dtype=torch.int32)  # noqa: E731
+    pages = torch.zeros(3, 2, 16, 64).to(torch.float8_e4m3fn)
+    scales = torch.zeros(3, 2, 2, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    q, last = (bf(2, 1, 4, 64), i32(2)) if call.startswith("decode") else (bf(5, 4, 64), i32(3))
+    stream = object()
+    ws = getattr(b, call)(q, pages, pages, scales, i32(2, 2), i32(2), last, q.clone(), 1.0, stream=stream)
+    assert made == [(stream, kind == "zeros")] and ws.numel() > 0
