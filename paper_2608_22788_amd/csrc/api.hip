@@ -95,16 +95,19 @@ struct Plan {
 // would allow 3: the third team lowers throughput by 8 %.  The auto count is further capped at launch by
 // the occupancy the HIP runtime reports for the compiled kernel, so all
 // workers run in one round.
-static int per_cu_bound(bool q1, bool team, int rows) {
+// A cache in 8 bits with three and more row blocks keeps the vector units busy rather
+// than memory: 4 there too (4 sequences of 32-98 thousand tokens, 64 rows: 148 against
+// 178 us with 3; 64 of 500-8,000: 178 against 216).
+static int per_cu_bound(bool q1, bool team, int rows, bool kv8 = false) {
     if (q1)
         return 4;
     if (team)
         return 2;
-    return rows <= 8 ? 4 : 3;
+    return rows <= 8 || (kv8 && rows > 32) ? 4 : 3;
 }
 
-static int auto_workers(const ts_attn_shape *s, bool q1, bool team, int rows) {
-    int64_t w = 256LL * per_cu_bound(q1, team, rows);
+static int auto_workers(const ts_attn_shape *s, bool q1, bool team, int rows, bool kv8 = false) {
+    int64_t w = 256LL * per_cu_bound(q1, team, rows, kv8);
     // Small shapes get fewer workers so that each has at least a few pages.
     const int64_t pages_ub = (int64_t)s->num_seqs * s->num_kv_heads *
                              ((s->max_ctx_len + kPage - 1) / kPage);
@@ -254,14 +257,14 @@ int make_plan(const ts_attn_shape *s, bool kv8, Plan *pl) {
     if (s->num_workers > 0)
         pl->W = s->num_workers;
     else
-        pl->W = pl->group ? group_workers(s, pl->rows_per_unit) : auto_workers(s, pl->q1, pl->team, pl->rows_per_unit);
+        pl->W = pl->group ? group_workers(s, pl->rows_per_unit) : auto_workers(s, pl->q1, pl->team, pl->rows_per_unit, kv8);
     // Workspace: the split counters first, at a fixed size whatever the shape,
     // so that no call's partial results ever land on them (they are zero
     // between calls); then 256 bytes for the TS_DEBUG check's flag word; then
     // the partial outputs and their log-sum-exp, with slots for as many workers
     // as single wavefronts would be where groups run: a caller's workspace for
     // TS_VARIANT_AUTO then also serves TS_VARIANT_WAVE with the same shape.
-    const int ws_workers = pl->group ? auto_workers(s, false, false, pl->rows_per_unit) : pl->W;
+    const int ws_workers = pl->group ? auto_workers(s, false, false, pl->rows_per_unit, kv8) : pl->W;
     const size_t slots = 2 * (size_t)ws_workers;
     pl->ws_cnt_off = 0;
     pl->ws_dbg_off = kCounterBytes;
