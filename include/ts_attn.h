@@ -411,7 +411,8 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *                     one for the values of each page and KV head
  * A cached value is code * 2^(byte - 127), exactly a bf16 number for the bytes 27
  * to 227 that ts_rope_append_kv8 writes (the powers 2^-100 to 2^100); with others
- * the product is taken as bf16 takes it.  Code 0x7f (and 0xff) is NaN; e4m3 has no
+ * from 1 to 254 the product is taken as bf16 takes it; 0 and 255 are not for pages
+ * that hold tokens.  Code 0x7f (and 0xff) is NaN; e4m3 has no
  * infinity. */
 
 /* ts_rope_append into the cache held in 8 bits.  Norm and rotation in float32 as
@@ -463,12 +464,13 @@ int ts_chunk_attn_kv8(const ts_chunk_shape *shape, const void *q, int64_t q_stri
  * penalties for tokens that its text holds, biases and a grammar's mask.  For
  * token v of row b with logit l, in float32 and in this order:
  *   x = l;
- *   v among the row's tokens:  x = x > 0 ? x / repetition : x * repetition;
+ *   v among the row's tokens:  x = x > 0 ? x * (1 / repetition) : x * repetition;
  *   v n > 0 times among those behind the prompt:
  *                              x = x - (frequency * n + presence);
  *   biases of v in the row's list:  x = x + their sum, added up in list order;
  *   v not allowed:             x = -inf;
- *   out = x, rounded once.  Infinite and NaN logits go the same way.
+ *   out = x, rounded once.  Infinite and NaN logits go the same way; what no rule
+ *   names is copied.
  * A row whose mask allows nothing is all -inf (ts_sample gives token -1 for it).
  *   logits, out  float32 or bf16 [num_seqs][vocab], each with its type and its rows
  *                row_stride / out_stride elements apart (at least vocab, any

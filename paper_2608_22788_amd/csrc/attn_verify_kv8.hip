@@ -12,8 +12,16 @@
 // for a dim, the order of the value product's operand: 16 byte permutations
 // instead of 32 for a step.
 //
-// What bounds it: bytes.  Matrix and vector instructions of a step take about a
-// third of the time in which its 8 KiB arrive.
+// What bounds it.  Long caches: bytes.  256 sequences of 500-8,000 tokens take 345 us
+// (2.18 GB, 6.3 TB/s; a gather of the same 2 KiB blocks that computes nothing reaches
+// 6.4-6.6), 8 sequences of 16-65 thousand with 4 rows each 107 us (5.96 TB/s).  Vector
+// instructions issue in 25 % of a busy CU's cycles, the matrix units are busy 9 %.
+// Two steps under way instead of one: no difference (346 against 348 us).
+// One sequence of 1,600: 10 us, the chain of the launch and the join of its pieces;
+// two pages per wavefront instead of four take 11.3 (more pieces).
+// 33 rows and more (64 rows, 4 sequences of 32-98 thousand tokens, 171 us, 2.95 TB/s):
+// vector instructions, as each row block has its own scores and weights.  The chunk
+// kernel takes 189 us for it, four wavefronts that share the rows of one page 296.
 #include "attn_verify.h"
 
 namespace tsattn {

@@ -52,6 +52,19 @@
 // 317 MB; 256 sequences of one token behind 1,000: 181 us for 1,057 MB, 5.8 TB/s.
 // One short chunk (37 tokens behind 2,011, 23 us): the chain of a launch, finding
 // the work, two tiles and the join of 16 pieces.
+//
+// The cache held in 8 bits (kv8_common.h).  The same kernel; only the tiles' way
+// differs: codes come to LDS as they are, four tiles deep, each wavefront turns the
+// page that it loaded into bf16 rows of a stage, in registers, two codes to an
+// instruction that takes the page's power along (exact), and two stages suffice.
+// Half of the bytes, and for each value half a conversion and an eighth of an LDS
+// store, 6 % of the time in bank conflicts.  A prompt of 8,192 tokens takes 548-555 us,
+// 990-1,004 TFLOP/s (543-563 from the bf16 cache on the same boxes), 16 ragged prompts
+// of up to 1,024 tokens 319 us, 32 mixed sequences 83 us for 138 MB: there the starts
+// of row tiles count, about 9 us each, in which nothing is left to overlap.  What
+// mattered, on the prompt: conversions by all wavefronts at the start of a step 585
+// us; the keys' wavefronts before and the values' after it 558; ids and powers of 64
+// tiles in a lane each 548.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -679,7 +692,7 @@ struct Chunk {
     // Of codes, a lane holds one of 64 tiles: the id of the wavefront's page and the
     // byte of its power, which reach their tile by lane reads.  (Scalar loads of them
     // tile by tile would make every wait for LDS a wait for memory, since both are
-    // counted together: 16 ragged sequences 321 us.)
+    // counted together: 16 ragged sequences 321 us instead of 313.)
     struct CodePages {
         const int32_t *pt;
         int first, last;   // as above

@@ -4,7 +4,7 @@
 // For token v of a row with logit l, with n the number of times that v is among
 // the row's answer (its tokens behind the prompt) and "seen" if it is among its
 // tokens at all, in float32 and in this order:
-//   x = l;  seen: x = x > 0 ? x / repetition : x * repetition;
+//   x = l;  seen: x = x > 0 ? x * (1 / repetition) : x * repetition;
 //   n > 0: x -= frequency * n + presence;  biased: x += the sum of v's biases;
 //   not allowed: x = -inf;  out = x, rounded once.
 //
@@ -14,7 +14,9 @@
 // have few thousands of them, and the slices of a row are neighbours on one XCD,
 // whose L2 holds them.  Its logits are on their way meanwhile.  Biases are added up
 // in LDS too, in the order of the list whatever threads they fall to: of the
-// threads that hold biases of one token, the first adds its own, then the next.
+// threads that hold biases of one token, the first adds its own, then the next
+// (three barriers for each, so a list that names one token over and over takes time
+// for every mention).
 // One launch, nothing kept in memory between slices or calls.
 //
 // In place, a thread that has nothing to change neither reads nor writes.
@@ -44,6 +46,7 @@ constexpr int kSlice = kThreads * kPer;
 constexpr int kAhead = 4;                      // groups of four text tokens whose loads are in flight together
 constexpr int kTable = kSlice + kWave;          // and a place for each lane's tokens of other slices
 constexpr uint32_t kInPrompt = 0x80000000u;
+constexpr uint32_t kNone = 0x80000000u;         // no bias: -0, which added changes nothing, +0 and -0 neither
 
 struct RulesParams {
     const void *logits;
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     for (int i = 0; i < kSlice / 4 / kThreads; i++) {
         zero[i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
         if (p.bias_tokens)
-            zero[kTable / 4 + i * kThreads + tid] = u32x4_t{0u, 0u, 0u, 0u};
+            zero[kTable / 4 + i * kThreads + tid] = u32x4_t{kNone, kNone, kNone, kNone};
     }
     lds_sync();
 
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
 #pragma unroll
     for (int e = 0; e < kPer; e += 4) {
         const u32x4_t cv = *reinterpret_cast<const u32x4_t *>(count + kPer * tid + e);
-        f32x4_t wv = {0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4_t wv = {-0.0f, -0.0f, -0.0f, -0.0f};
         if (p.bias_tokens)
             wv = *reinterpret_cast<const f32x4_t *>(bias + kPer * tid + e);
 #pragma unroll
@@ -332,9 +335,9 @@ int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, co
         return fail(TS_ERR_NULL, "penalties and lengths need tokens");
     if (tokens && !lens)
         return fail(TS_ERR_NULL, "tokens need lens");
-    if (tokens && (cfg->max_tokens < 0 || cfg->max_tokens > (1 << 30) || cfg->token_stride < cfg->max_tokens ||
+    if (tokens && (cfg->max_tokens < 0 || cfg->max_tokens > (1 << 29) || cfg->token_stride < cfg->max_tokens ||
                    cfg->token_stride > most))
-        return fail(TS_ERR_ARG, "max_tokens %d outside [0, 2^30], or token_stride %lld below it or above 2^40",
+        return fail(TS_ERR_ARG, "max_tokens %d outside [0, 2^29], or token_stride %lld below it or above 2^40",
                     cfg->max_tokens, (long long)cfg->token_stride);
     if (!bias_starts != !bias_tokens || !bias_starts != !bias_values)
         return fail(TS_ERR_NULL, "biases need starts, tokens and values");

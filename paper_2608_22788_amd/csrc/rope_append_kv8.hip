@@ -18,8 +18,15 @@
 // floor(q_starts[b] / 16) + 2 b on, which is room enough for any position of its
 // rows, and a workgroup finds its sequence among those closed sums.
 //
-// What bounds it: memory where there are many rows; the chain starts -> rows ->
-// maximum -> stores where there are few.
+// What bounds it.  Many rows: vector instructions, busy 81 % of the time beside the
+// bytes: 8,192 rows of 32/8 heads with norms take 50 us for 185 MB (3.7 TB/s; a large
+// copy of as many takes 38).  Rotation and norm of two values are about ten of them,
+// and nothing is worked out twice.  Norm weights in one factor with the angles, and a
+// conversion that divides by the power, brought 53 to 50.  Several KV heads to a
+// workgroup, which find their sequence and angles once, take 56 (2), 64 (4) and 73 us
+// (8): fewer loads are under way.  Bounds on registers for more wavefronts: 74 and 117
+// (spills).  Few rows: the chain starts -> lengths -> rows -> maximum -> stores, 6 us
+// for 8 of them.
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"

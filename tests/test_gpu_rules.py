@@ -1,9 +1,9 @@
 """GPU tests of the rules on logits against oracle/rules.py in float64.
 
-Tolerance: up to five float32 operations (a product or quotient, frequency * n, the
+Tolerance: up to six float32 operations (a reciprocal and a product, frequency * n, the
 sum with presence, the difference, the bias) and as many additions as a token has
 biases less one (at most 40 here), each off by 2^-24 of the largest magnitude met,
-so 45 * 2^-24 < 2^-18 of it; a bf16 result once more by 2^-8 of itself."""
+so 46 * 2^-24 < 2^-18 of it; a bf16 result once more by 2^-8 of itself."""
 import numpy as np
 import pytest
 
@@ -169,3 +169,21 @@ def test_rules_no_text_and_empty_lists():
                         bias_starts=torch.zeros(3, dtype=torch.int32, device="cuda"), bias_tokens=e(torch.int32),
                         bias_values=e(torch.float32))
     assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("types", ["ff", "bb", "bf"])
+def test_rules_copies_what_no_rule_names(types):
+    """Bit for bit, signed zeros and denormal values among them, with rules for
+    other tokens and without any."""
+    import torch
+    from paper_2608_22788_amd import binding
+    bf = {"f": torch.float32, "b": torch.bfloat16}
+    x = torch.randn(3, 5003, device="cuda").to(bf[types[0]])
+    x[:, ::7], x[:, 1::7], x[:, 2::7], x[:, 3::7] = -0.0, 0.0, -1e-39, float("-inf")
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    for kw in ({}, dict(bias_starts=i32([0, 1, 1, 2]), bias_tokens=i32([5002, 5002]), bias_values=torch.ones(2, device="cuda"))):
+        out = torch.zeros_like(x, dtype=bf[types[1]])
+        binding.logit_rules(x, out, **kw)
+        want, got = x.to(bf[types[1]])[:, :5002].contiguous(), out[:, :5002].contiguous()
+        bits = torch.int32 if types[1] == "f" else torch.int16
+        assert torch.equal(got.view(bits), want.view(bits)), kw.keys()
