@@ -755,6 +755,19 @@ struct Chunk {
         bool first = pc.us <= begin;   // the range starts inside it: its partial result's slot
         State st;
         set_addresses(st, lds, wave, lane);
+        // Queries of a piece: before its first tiles, and before the results of the
+        // piece in front of it, since loads and stores finish in order.
+        const auto queries = [&](const Piece &of) __attribute__((always_inline)) {
+            const SeqInfo sq = seq_info(p, of.b);
+            const int token = of.m * p.TT + r / p.G;
+            const bool row_ok = r < p.TT * p.G && token < sq.c.Q;
+            const int head = of.g * p.G + r % p.G;
+            const uint16_t *qr = p.q + (int64_t)(sq.row0 + (row_ok ? token : 0)) * p.q_stride + (int64_t)(row_ok ? head : 0) * D + 8 * h;
+#pragma unroll
+            for (int ks = 0; ks < kKSteps; ks++)
+                st.qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + 16 * ks) : u32x4_t{0u, 0u, 0u, 0u};
+        };
+        queries(pc);
         TilePages pages = start(p, st, pc, lds, wave, lane);
         for (;;) {
             const SeqInfo sq = seq_info(p, pc.b);
@@ -768,12 +781,9 @@ struct Chunk {
             st.lim = row_ok ? sq.L - sq.c.Q + token + 1 : 0;
             st.m_ref = kLowest;
             st.l = 0.0f;
-            const uint16_t *qr = p.q + (int64_t)(sq.row0 + (row_ok ? token : 0)) * p.q_stride + (int64_t)(row_ok ? head : 0) * D + 8 * h;
 #pragma unroll
-            for (int ks = 0; ks < kKSteps; ks++) {
-                st.qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + 16 * ks) : u32x4_t{0u, 0u, 0u, 0u};
+            for (int ks = 0; ks < kKSteps; ks++)
                 st.qf[ks] ^= p.q_sign;
-            }
 #pragma unroll
             for (int dt = 0; dt < kDTiles; dt++)
 #pragma unroll
@@ -888,8 +898,10 @@ struct Chunk {
             }
             Piece nx = pc;
             const bool more = next_piece(p, s_end, x, end, nx);
-            if (more)
+            if (more) {
+                queries(nx);
                 pages = start(p, st, nx, lds, wave, lane);
+            }
             if (row_ok)
                 write_rows(p, st, sq, pc, first ? 2 * w : 2 * w + 1, r, token, head, h);
             if (!more)
