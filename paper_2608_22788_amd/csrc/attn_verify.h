@@ -242,7 +242,8 @@ struct Verify {
     __device__ __forceinline__ static f32x4_t weigh(u32x2_t w, u32x2_t v, f32x4_t sum) {
         return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, w), __builtin_bit_cast(s16x4_t, v), sum, 0, 0, 0);
     }
-    __device__ static void page_step(const AttnParams &p, State &st, Kv8Regs &cur, int j,
+    template <typename Params>   // (AttnParams, or a chunk's)
+    __device__ static void page_step(const Params &p, State &st, Kv8Regs &cur, int j,
                                      int full_end, int seg_end_tok, int kq) {
         const int t0 = j * kPage;
         const bool masked = t0 + kStep * kPage > full_end;      // wavefront-uniform

@@ -58,13 +58,17 @@
 // page that it loaded into bf16 rows of a stage, in registers, two codes to an
 // instruction that takes the page's power along (exact), and two stages suffice.
 // Half of the bytes, and for each value half a conversion and an eighth of an LDS
-// store, 6 % of the time in bank conflicts.  A prompt of 8,192 tokens takes 548-555 us,
-// 990-1,004 TFLOP/s (543-563 from the bf16 cache on the same boxes), 16 ragged prompts
-// of up to 1,024 tokens 319 us, 32 mixed sequences 83 us for 138 MB: there the starts
-// of row tiles count, about 9 us each, in which nothing is left to overlap.  What
-// mattered, on the prompt: conversions by all wavefronts at the start of a step 585
+// store, 6 % of the time in bank conflicts.  A prompt of 8,192 tokens takes 546-565 us,
+// 973-1,007 TFLOP/s (538-563 from the bf16 cache on the same boxes), 16 ragged prompts
+// of up to 1,024 tokens 312-315 us.  What mattered, on the prompt: conversions by all wavefronts at the start of a step 585
 // us; the keys' wavefronts before and the values' after it 558; ids and powers of 64
 // tiles in a lane each 548.
+// Row tiles of up to 16 rows (decoding sequences) would have one busy wavefront of
+// eight and take 1.2 us a KV tile, as long as from the bf16 cache, whose bytes take
+// that long.  Their wavefronts share the keys instead (few_rows): 0.66 us, 6.3 TB/s
+// over the chip.  32 mixed sequences, 138 MB: 83 us without, 77 with the places of the
+// bf16 cache, 63 with those that the times of either kind ask for (chunk_partition.h).
+// Three steps under way for a wavefront instead of two spill registers: 79 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -72,6 +76,7 @@
 #include <type_traits>
 
 #include "attn_common.h"
+#include "attn_verify.h"
 #include "chunk_common.h"
 #include "chunk_partition.h"
 #include "kv8_common.h"
@@ -124,6 +129,7 @@ struct SeqInfo {
     int row0, L;
     ChunkSeq c;
 };
+template <bool k8>
 __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
     SeqInfo s;
     const int a = min(max(ld_meta(p.q_starts, b), 0), p.num_tokens);
@@ -134,6 +140,7 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
     s.c.P = max(s.L - s.c.Q, 0);
     s.c.TT = p.TT;
     s.c.G = p.G;
+    s.c.k8 = k8;
     return s;
 }
 
@@ -141,6 +148,7 @@ __device__ __forceinline__ SeqInfo seq_info(const ChunkParams &p, int b) {
 // thread per sequence, sums within wavefronts and then, past 64 sequences, over
 // them.  (With one wavefront for all of them a call of 4,096 sequences of 100
 // tokens took 113 us more; it takes 720.)
+template <bool k8>
 __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
     const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     uint64_t base = 0;
@@ -148,7 +156,7 @@ __device__ inline void tile_ends(const ChunkParams &p, uint64_t *s_end) {
         const int b = b0 + threadIdx.x;
         uint64_t n = 0;
         if (b < p.B) {
-            const SeqInfo s = seq_info(p, b);
+            const SeqInfo s = seq_info<k8>(p, b);
             n = s.c.Q > 0 ? (uint64_t)s.c.total() : 0;
         }
         const uint64_t incl = wave_incl_scan(n);
@@ -193,7 +201,7 @@ struct Piece {
 __device__ __forceinline__ void cut_piece(Piece &r, const ChunkSeq &c, int64_t from, int64_t range_end) {
     r.n = first_lane_int(c.cost(r.m));
     r.weight = first_lane_int(c.weight(r.m));
-    const int64_t unit_end = r.us + (int64_t)r.n * r.weight + kUnitPlaces;
+    const int64_t unit_end = r.us + (int64_t)r.n * r.weight + c.behind(r.m);
     r.next = unit_end < range_end ? unit_end : range_end;
     r.j0 = first_lane_int(min(tile_at(from - r.us, r.weight), r.n));
     r.j1 = first_lane_int(min(tile_at(r.next - r.us, r.weight), r.n));
@@ -202,6 +210,7 @@ __device__ __forceinline__ void cut_piece(Piece &r, const ChunkSeq &c, int64_t f
 
 // The unit that holds place x, and the part of it in [x, range_end).
 // Units are laid out sequence by sequence, head by head, row tile by row tile.
+template <bool k8>
 __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end, int64_t x, int64_t range_end) {
     const int lane = threadIdx.x & (kWave - 1);
     Piece r;
@@ -219,7 +228,7 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end,
     const int64_t off = x - pre * p.Hkv;
     r.g = first_lane_int((int)(off / per_head));
     const int64_t in_head = off - r.g * per_head;
-    const ChunkSeq c = seq_info(p, r.b).c;
+    const ChunkSeq c = seq_info<k8>(p, r.b).c;
     // the last row tile that starts at or before in_head
     int m = 0, span = c.tiles();
     while (span > 1) {
@@ -241,9 +250,10 @@ __device__ inline Piece locate_tile(const ChunkParams &p, const uint64_t *s_end,
 // The next piece with KV tiles at or behind x in a worker's range, false if
 // there is none.  `r` is the piece before it, whether it has tiles or not: the
 // row tiles of one head follow each other, so most of the time nothing is searched.
+template <bool k8>
 __device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t *s_end, int64_t &x, int64_t range_end, Piece &r) {
     while (x < range_end) {
-        const ChunkSeq c = seq_info(p, r.b).c;
+        const ChunkSeq c = seq_info<k8>(p, r.b).c;
         if (r.m + 1 < c.tiles() || r.g + 1 < p.Hkv) {
             const bool same = r.m + 1 < c.tiles();
             r.g = same ? r.g : r.g + 1;
@@ -251,7 +261,7 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, const uint64_t 
             r.us = x;
             cut_piece(r, c, x, range_end);
         } else {
-            r = locate_tile(p, s_end, x, range_end);
+            r = locate_tile<k8>(p, s_end, x, range_end);
         }
         x = r.next;
         if (r.j0 < r.j1)
@@ -713,7 +723,7 @@ struct Chunk {
     // Starts loading the first tiles of a piece.
     typedef std::conditional_t<k8, CodePages, Pages> TilePages;
     __device__ __forceinline__ static TilePages start(const ChunkParams &p, const State &st, const Piece &pc, char *lds, int wave, int lane) {
-        const SeqInfo sq = seq_info(p, pc.b);
+        const SeqInfo sq = seq_info<k8>(p, pc.b);
         TilePages pages{p.page_table + (size_t)pc.b * p.max_pages, first_lane_int(pc.j0 * kTilePages + wave % kTilePages),
                     first_lane_int((max(sq.L, 1) - 1) / kPage), sq.c.Q <= sq.c.TT};
         if constexpr (k8) {
@@ -736,6 +746,153 @@ struct Chunk {
     // or by the merge kernel (so the output may take the queries' place).
     // While a piece's result is written, the first tiles of
     // the next one are already on their way.
+    // ---- row tiles of up to 16 rows, of the cache held in 8 bits ------------------
+    // One wavefront has rows then, so the wavefronts take turns at the keys instead:
+    // wavefront w the pages 2 w, 2 w + 1 of every 16, in the steps of attn_verify.h,
+    // straight to registers, two steps ahead.  Their sums meet in LDS.
+    typedef Verify<D, 1, true> Few;
+    __device__ __forceinline__ static bool is_few(const ChunkParams &p, const Piece &pc) {
+        const SeqInfo sq = seq_info<k8>(p, pc.b);
+        return k8 && first_lane_int(min(p.TT, sq.c.Q - pc.m * p.TT) * p.G) <= kFewRows;
+    }
+    __device__ __forceinline__ static void few_rows(const ChunkParams &p, const Piece &pc, int slot, char *lds, int wave, int lane) {
+        constexpr int kFewPages = 2, kSteps = kWave / kFewPages, kRing = 2, VE = D / 16;
+        static_assert(Few::kStep == kFewPages, "pages of a step");
+        // (Unknown here, so that no address of this function is worked out in front of
+        // the loop over pieces and held through the other row tiles' steps.)
+        asm volatile("" : "+v"(lane));
+        const SeqInfo sq = seq_info<k8>(p, pc.b);
+        const int n = lane & 15, kq = lane >> 4;
+        const int rows = first_lane_int(min(p.TT, sq.c.Q - pc.m * p.TT) * p.G);
+        const int seg_end = first_lane_int(min(sq.L, pc.j1 * kKeyTile));
+        const int first_lim = first_lane_int(sq.L - sq.c.Q + pc.m * p.TT + 1);
+        const int first = pc.j0 * kTilePages, end = first_lane_int((max(seg_end, 0) + kPage - 1) / kPage);
+        const int steps = max(end - first + kFewPages - 1, 0) / kFewPages;
+        const int own = steps > wave ? (steps - wave + kChunkWaves - 1) / kChunkWaves : 0;
+        const auto page_of = [&](int s) { return first + kFewPages * (wave + kChunkWaves * s); };
+
+        // Page ids and powers of 32 steps, one page in a lane each.
+        const int32_t *pt = p.page_table + (size_t)pc.b * p.max_pages;
+        int ids = -1, powers = 0, later = 0x7f7f;
+        const auto fetch = [&](int s) __attribute__((always_inline)) {
+            const int page = page_of(s + lane / kFewPages) + lane % kFewPages;
+            ids = page < end ? pt[page] : -1;
+            ids = ids < p.num_pages ? ids : -1;
+            later = 0x7f7f;
+            if (ids >= 0)
+                later = *reinterpret_cast<const uint16_t *>(p.kv_scales + 2 * ((size_t)ids * p.Hkv + pc.g));
+        };
+        const auto load = [&](int s, typename Few::Kv8Regs &r) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < kFewPages; h++) {
+                const int pid = __builtin_amdgcn_readlane(ids, kFewPages * (s % kSteps) + h);
+                const size_t block = (size_t)max(pid, 0) * p.Hkv + pc.g;
+                const int bytes = pid >= 0 ? kPageBytes : 0;   // (no records: zeros)
+                const block_rsrc_t rk = block_rsrc(reinterpret_cast<const char *>(p.k_pages) + block * kPageBytes, bytes);
+                const block_rsrc_t rv = block_rsrc(reinterpret_cast<const char *>(p.v_pages) + block * kPageBytes, bytes);
+#pragma unroll
+                for (int e = 0; e < D / 64; e++)
+                    r.k[h][e] = ld_block16(rk, n * D + 16 * kq + 64 * e);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    r.v[h][i].load(rv, (4 * kq + i) * D + VE * n);
+            }
+        };
+
+        typename Few::State st;
+        typename Few::Kv8Regs ring[kRing];
+        const bool row_ok = n < rows;
+        const int token = pc.m * p.TT + (row_ok ? n / p.G : 0), head = pc.g * p.G + (row_ok ? n % p.G : 0);
+        const uint16_t *qr = p.q + (int64_t)(sq.row0 + token) * p.q_stride + (int64_t)head * D;
+        if (own > 0)
+            fetch(0);
+        u32x4_t qf[kKSteps / 2];
+#pragma unroll
+        for (int ks = 0; ks < kKSteps / 2; ks++)
+            qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + Few::q_dim(kq, ks)) : u32x4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < kRing - 1; i++)
+            if (i < own)
+                load(i, ring[i]);
+#pragma unroll
+        for (int ks = 0; ks < kKSteps / 2; ks++)
+            st.qf[0][ks] = __builtin_bit_cast(uint4, qf[ks] ^ p.q_sign);
+        powers = later;
+        const int full_end = min(first_lim, seg_end);
+        st.lim[0] = min(row_ok ? sq.L - sq.c.Q + token + 1 : sq.L, seg_end);
+        st.m_ref[0] = -INFINITY;
+        st.lacc[0] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int jj = 0; jj < VE; jj++)
+            st.acc[0][jj] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s0 = 0; s0 < own; s0 += kRing) {
+#pragma unroll
+            for (int i = 0; i < kRing; i++) {
+                const int s = s0 + i, next = s + kRing - 1;
+                if (s < own) {
+                    if (s > 0 && s % kSteps == 0)
+                        powers = later;
+                    if (next < own) {
+                        if (next % kSteps == 0)
+                            fetch(next);
+                        load(next, ring[(i + kRing - 1) % kRing]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < kFewPages; h++)
+                        ring[i].power[h] = __builtin_amdgcn_readlane(powers, kFewPages * (s % kSteps) + h);
+                    Few::page_step(p, st, ring[i], page_of(s), full_end, seg_end, kq);
+                }
+            }
+        }
+
+        // Sums and statistics of each wavefront, then a thread for four values of a row.
+        constexpr int kParts = VE / 4;
+        f32x4_t *const sums = reinterpret_cast<f32x4_t *>(lds);   // [wave][4][kParts][lane]
+        float *const stats = reinterpret_cast<float *>(lds + kCodes);   // [wave][2][16]
+        static_assert(kChunkWaves * 4 * kParts * kWave * 16 <= kCodes, "sums in front of the codes");
+        lds_barrier();   // nobody reads the piece in front of this one any more
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+#pragma unroll
+            for (int e = 0; e < kParts; e++)
+                sums[((wave * 4 + i) * kParts + e) * kWave + lane] =
+                    f32x4_t{st.acc[0][4 * e][i], st.acc[0][4 * e + 1][i], st.acc[0][4 * e + 2][i], st.acc[0][4 * e + 3][i]};
+            if (n == 0)
+                stats[32 * wave + 16 + 4 * kq + i] = st.lacc[0][i];
+        }
+        if (kq == 0)
+            stats[32 * wave + n] = st.m_ref[0];
+        lds_barrier();
+        const int tid = wave * kWave + lane, part = tid & 15, e = (tid >> 4) % kParts, r = tid / (16 * kParts);
+        if (r < rows) {   // (of 16 or 32)
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kChunkWaves; k++)
+                m = fmaxf(m, stats[32 * k + r]);
+            f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kChunkWaves; k++) {
+                const float mk = stats[32 * k + r];
+                const float f = mk == -INFINITY ? 0.0f : fast_exp2(mk - m);
+                l += f * stats[32 * k + 16 + r];
+                x += f * sums[((k * 4 + (r & 3)) * kParts + e) * kWave + 16 * (r >> 2) + part];
+            }
+            const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // NaN stays
+            x *= inv;
+            const int dim = VE * part + 4 * e;
+            if (pc.whole) {
+                uint16_t *dst = p.out + (int64_t)(sq.row0 + pc.m * p.TT + r / p.G) * p.out_stride + (int64_t)(pc.g * p.G + r % p.G) * D + dim;
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+            } else {
+                const int64_t row = (int64_t)slot * kTileRows + r;
+                *reinterpret_cast<f32x4_t *>(p.ws_o + row * D + dim) = x;
+                if (part == 0 && e == 0)
+                    p.ws_lse[row] = l == 0.0f ? -INFINITY : l > 0.0f ? m + __log2f(l) : l;
+            }
+        }
+        lds_barrier();
+    }
+
     __device__ __forceinline__ static void work(const ChunkParams &p, const uint64_t *s_end, int w, int64_t begin, int64_t end, char *lds) {
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = first_lane_int(threadIdx.x / kWave);
@@ -743,14 +900,14 @@ struct Chunk {
         const int r = wave * kRowBlock + (lane & 31);
         if (begin >= end)
             return;
-        Piece pc = locate_tile(p, s_end, begin, end);
+        Piece pc = locate_tile<k8>(p, s_end, begin, end);
         int64_t x = pc.next;
         if (threadIdx.x == 0) {
-            const SeqInfo sq = seq_info(p, pc.b);
+            const SeqInfo sq = seq_info<k8>(p, pc.b);
             const int at = pc.m * p.TT;
             p.cuts[w] = Cut{(int64_t)s_end[p.B - 1] * p.Hkv, pc.us, pc.n, pc.weight, sq.row0 + at, min(p.TT, sq.c.Q - at), pc.g * p.G};
         }
-        if (pc.j0 >= pc.j1 && !next_piece(p, s_end, x, end, pc))
+        if (pc.j0 >= pc.j1 && !next_piece<k8>(p, s_end, x, end, pc))
             return;
         bool first = pc.us <= begin;   // the range starts inside it: its partial result's slot
         State st;
@@ -758,7 +915,7 @@ struct Chunk {
         // Queries of a piece: before its first tiles, and before the results of the
         // piece in front of it, since loads and stores finish in order.
         const auto queries = [&](const Piece &of) __attribute__((always_inline)) {
-            const SeqInfo sq = seq_info(p, of.b);
+            const SeqInfo sq = seq_info<k8>(p, of.b);
             const int token = of.m * p.TT + r / p.G;
             const bool row_ok = r < p.TT * p.G && token < sq.c.Q;
             const int head = of.g * p.G + r % p.G;
@@ -767,10 +924,33 @@ struct Chunk {
             for (int ks = 0; ks < kKSteps; ks++)
                 st.qf[ks] = row_ok ? *reinterpret_cast<const u32x4_t *>(qr + 16 * ks) : u32x4_t{0u, 0u, 0u, 0u};
         };
-        queries(pc);
-        TilePages pages = start(p, st, pc, lds, wave, lane);
+        bool few = is_few(p, pc);
+        TilePages pages;
+        if (!few) {
+            queries(pc);
+            pages = start(p, st, pc, lds, wave, lane);
+        }
         for (;;) {
-            const SeqInfo sq = seq_info(p, pc.b);
+            if constexpr (k8) {
+                if (few) {
+                    few_rows(p, pc, first ? 2 * w : 2 * w + 1, lds, wave, lane);
+                    if (!next_piece<k8>(p, s_end, x, end, pc))
+                        return;
+                    first = false;
+                    few = is_few(p, pc);
+                    if (!few) {
+                        queries(pc);
+                        pages = start(p, st, pc, lds, wave, lane);
+                    } else {   // (nothing to keep meanwhile)
+#pragma unroll
+                        for (int ks = 0; ks < kKSteps; ks++)
+                            st.qf[ks] = u32x4_t{0u, 0u, 0u, 0u};
+                        pages = {};
+                    }
+                    continue;
+                }
+            }
+            const SeqInfo sq = seq_info<k8>(p, pc.b);
             const int token = pc.m * p.TT + r / p.G;
             const bool row_ok = r < p.TT * p.G && token < sq.c.Q;
             const int head = pc.g * p.G + r % p.G;
@@ -897,8 +1077,9 @@ struct Chunk {
                     add_odd(p, st, p.page_table + (size_t)pc.b * p.max_pages, pc.g, plain * kKeyTile, min(pc.j1 * kKeyTile, sq.L), h);
             }
             Piece nx = pc;
-            const bool more = next_piece(p, s_end, x, end, nx);
-            if (more) {
+            const bool more = next_piece<k8>(p, s_end, x, end, nx);
+            few = more && is_few(p, nx);
+            if (more && !few) {
                 queries(nx);
                 pages = start(p, st, nx, lds, wave, lane);
             }
@@ -947,7 +1128,7 @@ template <int D, bool k8>
 __global__ __launch_bounds__(kChunkWaves * kWave, 2) void chunk_attn_kernel(ChunkParams p) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // the tiles, then the prefix
     uint64_t *s_tiles = reinterpret_cast<uint64_t *>(lds + Chunk<D, k8>::kLds);
-    tile_ends(p, s_tiles);
+    tile_ends<k8>(p, s_tiles);
     const int64_t ptot = first_lane_int64((int64_t)s_tiles[p.B - 1]) * p.Hkv;
     const int w = xcd_worker(blockIdx.x, p.W);
     const int64_t begin = first_lane_int64(range_start(ptot, w, p.W, p.range_inv));
@@ -1054,7 +1235,7 @@ struct ChunkPlan {
     size_t ws_lse_off, ws_cut_off, ws_bytes;
 };
 
-int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
+int make_chunk_plan(const ts_chunk_shape *s, bool k8, ChunkPlan *pl) {
     const int st = check_chunk_shape(s);
     if (st)
         return st;
@@ -1064,7 +1245,7 @@ int make_chunk_plan(const ts_chunk_shape *s, ChunkPlan *pl) {
     const int64_t tiles = ((int64_t)s->num_tokens / pl->TT + std::min(s->num_seqs, s->num_tokens)) * s->num_kv_heads *
                           (((int64_t)s->max_ctx_len + kKeyTile - 1) / kKeyTile);
     const int64_t most = workers_bound(places_bound(s->num_seqs, s->num_kv_heads, s->num_tokens, pl->TT,
-                                                    (int64_t)s->max_pages_per_seq * kPage));
+                                                    (int64_t)s->max_pages_per_seq * kPage, k8));
     if (s->num_workers > most)
         return fail(TS_ERR_SHAPE, "num_workers %d exceeds %lld, what this shape's work can be cut into", s->num_workers,
                     (long long)most);
@@ -1124,7 +1305,7 @@ static int launch_chunk(const ts_chunk_shape *s, const void *q, int64_t q_stride
                         size_t workspace_bytes, void *stream) {
     clear_error();
     ChunkPlan pl;
-    int st = make_chunk_plan(s, &pl);
+    int st = make_chunk_plan(s, k8, &pl);
     if (st)
         return st;
     if (s->num_tokens == 0)
@@ -1202,10 +1383,14 @@ extern "C" {
 size_t ts_chunk_attn_workspace_size(const ts_chunk_shape *s) {
     clear_error();
     ChunkPlan pl;
-    return make_chunk_plan(s, &pl) == TS_OK ? pl.ws_bytes : 0;
+    return make_chunk_plan(s, false, &pl) == TS_OK ? pl.ws_bytes : 0;
 }
 
-size_t ts_chunk_attn_kv8_workspace_size(const ts_chunk_shape *s) { return ts_chunk_attn_workspace_size(s); }
+size_t ts_chunk_attn_kv8_workspace_size(const ts_chunk_shape *s) {
+    clear_error();
+    ChunkPlan pl;
+    return make_chunk_plan(s, true, &pl) == TS_OK ? pl.ws_bytes : 0;
+}
 
 int ts_chunk_attn(const ts_chunk_shape *s, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
                   const int32_t *page_table, const int32_t *ctx_lens, const int32_t *q_starts, void *out,

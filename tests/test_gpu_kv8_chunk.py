@@ -154,6 +154,41 @@ def test_many_sequences_and_pieces():
         check(make8((2, 1, D), [1] * 4096, [0] * 4096, seed=22), f"chunk8 4096 sequences, head_dim {D}")
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (16, 1, 128), (8, 2, 64), (5, 5, 64)], ids=str)
+def test_few_rows_behind_long_contexts(heads):
+    """Row tiles of up to 16 rows, whose wavefronts share the keys, beside larger
+    ones: more pages than a wavefront keeps the ids of, and each end of a page."""
+    few = max(16 * heads[1] // heads[0], 1)
+    s = make8(heads, [1, few, few + 1, 1, 2, 300, 1], [20000, 8191, 8192, 8193, 32, 40, 0], seed=31)
+    ref = reference(s)
+    for workers in (0, 1, 2, 7, 300):
+        check(s, f"chunk8 few rows {heads}", ref, num_workers=workers)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_few_rows_odd_values_and_pages(D):
+    """NaN codes that one of a few rows sees, bad pages, rows in front of position zero."""
+    import torch
+    s = make8((8, 2, D), [4, 2, 3, 4], [700, 29, 9000, 0], seed=32)
+    tab = s["table"].cpu().numpy()
+
+    def plant(name, b, t, g, d):
+        s[name].view(torch.uint8)[int(tab[b, t // 16]), g, t % 16, d] = NAN
+
+    plant("v_pages", 0, 703, 0, 3)       # the last row's own
+    plant("v_pages", 0, 701, 1, slice(0, D))
+    plant("k_pages", 0, 702, 1, 9)
+    plant("v_pages", 1, 30, 0, 5)
+    plant("v_pages", 2, 40, 1, D - 1)    # seen by every row
+    s["table"][2, 100:500:7] = -1
+    s["table"][2, 3] = s["k_pages"].shape[0]
+    s["ctx"][3] = 2                      # two rows have no key
+    ref = reference(s)
+    assert np.isnan(ref[0]).any() and not np.isnan(ref[0]).all()
+    for workers in (0, 1, 3, 50):
+        check(s, f"chunk8 few rows, odd values {D}", ref, num_workers=workers)
+
+
 def test_pages_behind_4_gib():
     import torch
     s = make8((32, 8, 128), [20, 1], [150, 40], seed=8)

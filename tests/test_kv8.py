@@ -1,6 +1,8 @@
 """The operators over the cache held in 8 bits without a GPU: their refusals
 before any HIP call, and the oracle's e4m3 against torch's."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -9,7 +11,7 @@ import torch
 from oracle import kv8
 from paper_2608_22788_amd import binding as b
 from test_abi import base_shape
-from test_chunk import BAD_SHAPES, config, shape
+from test_chunk import BAD_SHAPES, ROOT, config, shape
 
 
 def append(s, cfg, q=16, k=16, v=16, out=16, kp=16, vp=16, scales=16, table=16, ctx=16, starts=16, freq=16, qn=None,
@@ -194,3 +196,44 @@ def test_own_workspaces_are_made_on_the_calls_stream(monkeypatch, call, kind):
     stream = object()
     ws = getattr(b, call)(q, pages, pages, scales, i32(2, 2), i32(2), last, q.clone(), 1.0, stream=stream)
     assert made == [(stream, kind == "zeros")] and ws.numel() > 0
+
+
+PARTITION = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "chunk_partition.h"
+using namespace tsattn;
+int main() {
+    srand(11);
+    for (int it = 0; it < 20000; it++) {
+        ChunkSeq s;
+        s.k8 = true;
+        s.G = 1 + rand() % 16;
+        s.TT = kTileRows / s.G;
+        s.Q = 1 + rand() % (it % 2 ? 40 : 3000);
+        s.P = rand() % (it % 3 ? 100 : 1000000);
+        int64_t c = 0;
+        for (int j = 0; j < s.tiles(); j++) {
+            if (s.before(j) != c) { printf("before(%d): Q %d P %d G %d\n", j, s.Q, s.P, s.G); return 1; }
+            const int rows = s.tokens(j) * s.G;
+            c += (int64_t)s.cost(j) * (rows <= 16 ? 1 : rows <= 128 ? 2 : 3) + (rows <= 16 ? 8 : 20);
+        }
+        if (s.total() != c) return 2;
+        if (c > places_bound(1, 1, s.Q, s.TT, (int64_t)s.P + s.Q, true)) return 3;
+    }
+    for (int G = 1; G <= 16; G++)
+        if (places_bound(4096, 1024 / G, 1 << 22, kTileRows / G, 1ll << 30, true) >> 62) return 4;
+    printf("ok\n");
+    return 0;
+}
+"""
+
+
+def test_partition_arithmetic(tmp_path):
+    """Places of row tiles with the weights of this cache, against plain sums."""
+    src, exe = tmp_path / "p.cpp", tmp_path / "p"
+    src.write_text(PARTITION)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2608_22788_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.startswith("ok"), r.stdout + str(r.returncode)
