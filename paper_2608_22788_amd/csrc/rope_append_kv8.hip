@@ -49,7 +49,7 @@ struct Rope8Params {
     const float *inv_freq;
     const uint16_t *q_norm, *k_norm; // [D] or NULL
     int64_t q_stride, k_stride, v_stride, q_out_stride, num_pages;
-    int B, Hq, Hkv, G, max_pages, rot, interleaved, num_tokens;
+    int B, Hq, Hkv, G, max_pages, rot, num_tokens;
     float eps;
 };
 
@@ -87,7 +87,7 @@ __device__ __forceinline__ uint32_t max_wave(uint32_t x) {
     return max(h[0], h[1]);
 }
 
-template <int D>
+template <int D, bool kInterleaved>
 __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Params p) {
     constexpr int kLanes = D / 8;                  // lanes per head
     constexpr int kWaves = kPage * kLanes / kWave;
@@ -110,7 +110,22 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
     const bool active = pos >= P && pos < L;
     const int64_t row = first + (active ? pos - P : 0);
 
-    // rows, which do not depend on the page, then the page
+    // This lane's pairs: (x_j, x_{j + rot / 2}) with the partner lane `other`, j =
+    // 8 (c mod pieces) + e; interleaved, (x_{2 j}, x_{2 j + 1}), j = 4 c + e.  The
+    // two lanes of a half-split pair work out four of the eight angles each.
+    const int pieces = p.rot / 16;                 // pieces of each half
+    const bool upper = !kInterleaved && c >= pieces;
+    const int other = kInterleaved ? c : c < pieces ? c + pieces : c < 2 * pieces ? c - pieces : c;
+    const bool turns_here = 8 * c < p.rot;
+
+    // frequencies and rows, which do not depend on the page, then the page
+    struct __attribute__((packed, aligned(4))) Freqs {
+        float x[4];
+    } freq = {};
+    if (p.rot > 0) {
+        const int j = kInterleaved ? 4 * c : upper ? 8 * (c - pieces) + 4 : 8 * c;
+        freq = *reinterpret_cast<const Freqs *>(p.inv_freq + (turns_here ? j : 0));   // (rot is 16 or more)
+    }
     const auto load = [&](const uint16_t *x, int64_t stride, int h) {
         return active ? *reinterpret_cast<const u32x4_t *>(x + row * stride + (int64_t)h * D + 8 * c) : u32x4_t{0u, 0u, 0u, 0u};
     };
@@ -138,27 +153,17 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
         }
     }
 
-    // This lane's pairs: (x_j, x_{j + rot / 2}) with the partner lane `other`, j =
-    // 8 (c mod pieces) + e; interleaved, (x_{2 j}, x_{2 j + 1}), j = 4 c + e.  The
-    // two lanes of a half-split pair work out four of the eight angles each.
-    const int pieces = p.rot / 16;                 // pieces of each half
-    const bool upper = !p.interleaved && c >= pieces;
-    const int other = p.interleaved ? c : c < pieces ? c + pieces : c < 2 * pieces ? c - pieces : c;
-    const bool turns_here = 8 * c < p.rot;
     float co[8], si[8];                            // interleaved: of pair e / 2
     const auto angles = [&]() __attribute__((always_inline)) {
-        const int j = p.interleaved ? 4 * c : upper ? 8 * (c - pieces) + 4 : 8 * c;
         float mc[4], ms[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            mc[e] = 1.0f;
-            ms[e] = 0.0f;
-            if (turns_here) {
-                const double turns = (double)pos * (double)p.inv_freq[j + e] * 0.15915494309189533577;   // 1 / 2 pi
-                sincospif((float)(2.0 * (turns - rint(turns))), &ms[e], &mc[e]);
-            }
+            const double turns = (double)pos * (double)freq.x[e] * 0.15915494309189533577;   // 1 / 2 pi
+            sincospif((float)(2.0 * (turns - rint(turns))), &ms[e], &mc[e]);
+            mc[e] = turns_here ? mc[e] : 1.0f;
+            ms[e] = turns_here ? ms[e] : 0.0f;
         }
-        if (p.interleaved) {
+        if (kInterleaved) {
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 co[e] = mc[e / 2];
@@ -186,14 +191,14 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             a[e] = w ? wx[e] * co[e] : co[e];
-            b[e] = w ? (p.interleaved ? wx[e ^ 1] : wz[e]) * si[e] : si[e];
+            b[e] = w ? (kInterleaved ? wx[e ^ 1] : wz[e]) * si[e] : si[e];
         }
     };
     const auto turned = [&](u32x4_t raw, bool norm, const float a[8], const float b[8], float x[8]) __attribute__((always_inline)) {
         u32x4_t raw2;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            raw2[e] = p.interleaved ? raw[e] << 16 | raw[e] >> 16 : __shfl(raw[e], lane - c + other, kWave);
+            raw2[e] = kInterleaved ? raw[e] << 16 | raw[e] >> 16 : __shfl(raw[e], lane - c + other, kWave);
             raw2[e] = turns_here ? raw2[e] : 0;    // (an infinite value times a sine of zero)
         }
         float z[8];
@@ -350,10 +355,10 @@ int ts_rope_append_kv8(const ts_chunk_shape *s, const ts_rope_config *cfg, const
     p.max_pages = s->max_pages_per_seq;
     p.num_tokens = s->num_tokens;
     p.rot = cfg->rot_dim;
-    p.interleaved = cfg->interleaved;
     p.eps = cfg->eps;
     const int D = s->head_dim;
-    const auto kernel = D == 64 ? rope_append_kv8_kernel<64> : rope_append_kv8_kernel<128>;
+    const auto kernel = D == 64 ? cfg->interleaved ? rope_append_kv8_kernel<64, true> : rope_append_kv8_kernel<64, false>
+                                : cfg->interleaved ? rope_append_kv8_kernel<128, true> : rope_append_kv8_kernel<128, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(s->num_tokens / kPage + 2 * s->num_seqs), (unsigned)s->num_kv_heads),
                        dim3((unsigned)(kPage * D / 8)), 0, reinterpret_cast<hipStream_t>(stream), p);
     const hipError_t e = hipGetLastError();
