@@ -87,6 +87,20 @@ __device__ __forceinline__ uint32_t max_wave(uint32_t x) {
     return max(h[0], h[1]);
 }
 
+// Sine and cosine of f turns, |f| <= 1/2: of the angle's distance from the nearest
+// quarter, |x| <= pi / 4, by their series up to x^9 and x^8 (what follows is below
+// 2^-28 and 2^-25), exchanged and signed by the quarter.
+__device__ __forceinline__ void sincos_turns(float f, float *sine, float *cosine) {
+    const float quarter = rintf(4.0f * f);
+    const float x = fmaf(-0.25f, quarter, f) * 6.283185307179586f, z = x * x;   // (the difference is exact)
+    const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), x);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 40320.0f, -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
+    const int n = (int)quarter;
+    const uint32_t a = __float_as_uint(n & 1 ? c : s), b = __float_as_uint(n & 1 ? s : c);
+    *sine = __uint_as_float(a ^ ((uint32_t)n << 30 & 0x80000000u));
+    *cosine = __uint_as_float(b ^ ((uint32_t)(n + 1) << 30 & 0x80000000u));
+}
+
 template <int D, bool kInterleaved>
 __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Params p) {
     constexpr int kLanes = D / 8;                  // lanes per head
@@ -126,8 +140,9 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
         const int j = kInterleaved ? 4 * c : upper ? 8 * (c - pieces) + 4 : 8 * c;
         freq = *reinterpret_cast<const Freqs *>(p.inv_freq + (turns_here ? j : 0));   // (rot is 16 or more)
     }
+    // (lanes without a row read the first one)
     const auto load = [&](const uint16_t *x, int64_t stride, int h) {
-        return active ? *reinterpret_cast<const u32x4_t *>(x + row * stride + (int64_t)h * D + 8 * c) : u32x4_t{0u, 0u, 0u, 0u};
+        return *reinterpret_cast<const u32x4_t *>(x + row * stride + (int64_t)h * D + 8 * c);
     };
     const u32x4_t raw_k = load(p.k, p.k_stride, g), raw_v = load(p.v, p.v_stride, g);
     u32x4_t raw_q[kQueries];
@@ -159,7 +174,7 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const double turns = (double)pos * (double)freq.x[e] * 0.15915494309189533577;   // 1 / 2 pi
-            sincospif((float)(2.0 * (turns - rint(turns))), &ms[e], &mc[e]);
+            sincos_turns((float)(turns - rint(turns)), &ms[e], &mc[e]);
             mc[e] = turns_here ? mc[e] : 1.0f;
             ms[e] = turns_here ? ms[e] : 0.0f;
         }
@@ -225,11 +240,11 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
         turned(raw_k, p.k_norm, a, f, xk);
         float xv[8];
         unpack8(raw_v, xv);
-        const uint32_t mk = max_wave(active ? max_abs8(xk) : 0), mv = max_wave(max_abs8(xv));
+        const uint32_t mk = max_wave(active ? max_abs8(xk) : 0), mv = max_wave(active ? max_abs8(xv) : 0);
         uint32_t fk = mk, fv = mv;
         if (__builtin_expect(max(mk, mv) >= 0x7f800000u, 0)) {
             fk = max_wave(active ? max_finite8(xk) : 0);
-            fv = max_wave(max_finite8(xv));
+            fv = max_wave(active ? max_finite8(xv) : 0);
         }
         if (lane == 0) {
             s_max[0][wave] = mk;
