@@ -140,6 +140,19 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
         const int j = kInterleaved ? 4 * c : upper ? 8 * (c - pieces) + 4 : 8 * c;
         freq = *reinterpret_cast<const Freqs *>(p.inv_freq + (turns_here ? j : 0));   // (rot is 16 or more)
     }
+    struct Weights {
+        u32x4_t own, partner;
+    };
+    const auto weights = [&](const uint16_t *w) {
+        Weights r = {};
+        if (w) {
+            r.own = *reinterpret_cast<const u32x4_t *>(w + 8 * c);
+            if constexpr (!kInterleaved)
+                r.partner = *reinterpret_cast<const u32x4_t *>(w + 8 * other);
+        }
+        return r;
+    };
+    const Weights k_weights = weights(p.k_norm), q_weights = weights(p.q_norm);
     // (lanes without a row read the first one)
     const auto load = [&](const uint16_t *x, int64_t stride, int h) {
         return *reinterpret_cast<const u32x4_t *>(x + row * stride + (int64_t)h * D + 8 * c);
@@ -197,12 +210,10 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
     };
     // A head's value is r (x a + z b), z its partner in the pair and r its norm's
     // factor, with the norm's weights in a and b.
-    const auto factors = [&](const uint16_t *w, float a[8], float b[8]) __attribute__((always_inline)) {
+    const auto factors = [&](const uint16_t *w, const Weights &raw, float a[8], float b[8]) __attribute__((always_inline)) {
         float wx[8], wz[8];
-        if (w) {
-            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * c), wx);
-            unpack8(*reinterpret_cast<const u32x4_t *>(w + 8 * other), wz);
-        }
+        unpack8(raw.own, wx);
+        unpack8(raw.partner, wz);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             a[e] = w ? wx[e] * co[e] : co[e];
@@ -236,7 +247,7 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
     float xk[8], a[8], f[8];
     if (busy) {
         angles();
-        factors(p.k_norm, a, f);
+        factors(p.k_norm, k_weights, a, f);
         turned(raw_k, p.k_norm, a, f, xk);
         float xv[8];
         unpack8(raw_v, xv);
@@ -301,7 +312,7 @@ __global__ __launch_bounds__(kPage * D / 8) void rope_append_kv8_kernel(Rope8Par
     if (!busy)
         return;
     if (p.q_norm || p.k_norm)
-        factors(p.q_norm, a, f);
+        factors(p.q_norm, q_weights, a, f);
     for (int h0 = 0;;) {
 #pragma unroll
         for (int i = 0; i < kQueries; i++) {
