@@ -516,16 +516,15 @@ def spec_accept(p_target, q_draft, draft_tokens, num_draft, u_accept, u_sample, 
 # The smallest of these calls run for less than Python takes to check their
 # arguments attribute by attribute, so each attribute is read once.
 
-_BF16, _I32 = torch.bfloat16, torch.int32
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
 def _rows(t, name: str):
     """(tokens, heads, head_dim, row stride) of a packed token tensor, whose
     heads are contiguous."""
-    if t.dtype is _BF16 and t.dim() == 3:
-        T, H, D = t.shape
-        if t.is_contiguous():
-            return T, H, D, H * D
+    shape = t.shape
+    if t.dtype is _BF16 and len(shape) == 3:
+        T, H, D = shape
         row, head, value = t.stride()
         if value == 1 and (head == D or H == 1):
             # the stride of a single row is never used; torch may report any value
@@ -544,7 +543,7 @@ def _paged(k_pages, v_pages, page_table, ctx_lens, q_starts, dtype=_BF16):
     pool, table = k_pages.shape, page_table.shape
     if len(pool) != 4 or v_pages.shape != pool:
         raise ValueError("k_pages and v_pages must be [num_pages][kv_heads][16][head_dim], of one shape")
-    if len(table) != 2 or ctx_lens.shape != table[:1] or q_starts.shape != (table[0] + 1,):
+    if len(table) != 2 or ctx_lens.shape != (table[0],) or q_starts.shape != (table[0] + 1,):
         raise ValueError("page_table must be [B][max_pages], ctx_lens [B] and q_starts [B + 1]")
     return (*pool, *table)
 
@@ -607,11 +606,11 @@ def _rope_args(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts,
     rot = 0
     if inv_freq is not None:
         rot = 2 * inv_freq.numel()
-        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        if inv_freq.dtype is not _F32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous float32 vector")
-    for n, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if w is not None and (w.dtype != torch.bfloat16 or w.shape != (D,) or not w.is_contiguous()):
-            raise ValueError(f"{n} must be a contiguous bf16 vector of head_dim values")
+    for w in (q_norm, k_norm):
+        if w is not None and (w.dtype is not _BF16 or w.shape != (D,) or not w.is_contiguous()):
+            raise ValueError("q_norm and k_norm must be contiguous bf16 vectors of head_dim values")
     _check_device(q, k, v, q_out, k_pages, v_pages, page_table, ctx_lens, q_starts, inv_freq, q_norm, k_norm,
                   *others, stream=stream)
     return (ChunkShape(B, T, Hq, Hkv, D, P, T, maxp, maxp * P, 0, NP),
@@ -644,7 +643,9 @@ _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 def _check_scales(kv_scales, k_pages) -> None:
-    if kv_scales.dtype is not _E8M0 or kv_scales.shape != (*k_pages.shape[:2], 2) or not kv_scales.is_contiguous():
+    pool = k_pages.shape
+    if (kv_scales.dtype is not _E8M0 or len(pool) != 4 or kv_scales.shape != (pool[0], pool[1], 2) or
+            not kv_scales.is_contiguous()):
         raise ValueError(f"kv_scales must be a contiguous {_E8M0} tensor [num_pages][kv_heads][2]")
 
 
@@ -737,27 +738,31 @@ def logit_rules(logits, out, tokens=None, lens=None, prompt_lens=None, repetitio
     prompt_lens int32 [B], penalties float32 [B], bias_starts int32 [B + 1] with
     bias_tokens int32 and bias_values float32 [M], allowed int32 [B][ceil(V / 32)]
     (bits; rows may be strided); all but logits and out may be None."""
-    for name, t in (("logits", logits), ("out", out)):
-        if t.dtype not in _LOGITS or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name} must be a float32 or bf16 tensor [B][V] whose rows are contiguous")
-    B, V = logits.shape
-    if out.shape != logits.shape:
-        raise ValueError("out must have the shape of logits")
-    cfg = RulesConfig(B, V, _LOGITS[logits.dtype], _LOGITS[out.dtype], 0, 0, logits.stride(0) if B > 1 else V,
-                      out.stride(0) if B > 1 else V, 0, 0)
-    for name, t, dt, n in (("lens", lens, _I32, B), ("prompt_lens", prompt_lens, _I32, B),
-                           ("repetition", repetition, torch.float32, B), ("frequency", frequency, torch.float32, B),
-                           ("presence", presence, torch.float32, B), ("bias_starts", bias_starts, _I32, B + 1)):
-        if t is not None and (t.dtype is not dt or t.shape != (n,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {dt} vector of {n} values")
+    kind, out_kind, shape, strides, out_strides = (_LOGITS.get(logits.dtype), _LOGITS.get(out.dtype), logits.shape,
+                                                   logits.stride(), out.stride())
+    if len(shape) != 2 or out.shape != shape:
+        raise ValueError("logits must be [B][V], and out must have the shape of logits")
+    B, V = shape
+    if kind is None or out_kind is None or (V > 1 and (strides[1] != 1 or out_strides[1] != 1)):
+        raise ValueError("logits and out must be float32 or bf16 tensors [B][V] whose rows are contiguous")
+    cfg = RulesConfig(B, V, kind, out_kind, 0, 0, strides[0] if B > 1 else V, out_strides[0] if B > 1 else V, 0, 0)
+    rows = (B,)
+    for t, dt in ((lens, _I32), (prompt_lens, _I32), (repetition, _F32), (frequency, _F32), (presence, _F32)):
+        if t is not None and (t.dtype is not dt or t.shape != rows or not t.is_contiguous()):
+            raise ValueError("lens and prompt_lens must be contiguous int32 vectors, repetition, frequency and presence "
+                             "contiguous float32 vectors, with a value per row")
+    if bias_starts is not None and (bias_starts.dtype is not _I32 or bias_starts.shape != (B + 1,) or
+                                    not bias_starts.is_contiguous()):
+        raise ValueError(f"bias_starts must be a contiguous int32 vector of {B + 1} values")
     if tokens is not None:
-        if tokens.dtype is not _I32 or tokens.dim() != 2 or tokens.shape[0] != B or (tokens.shape[1] > 1 and tokens.stride(1) != 1):
+        shape, strides = tokens.shape, tokens.stride()
+        if tokens.dtype is not _I32 or len(shape) != 2 or shape[0] != B or (shape[1] > 1 and strides[1] != 1):
             raise ValueError("tokens must be an int32 tensor [B][N] whose rows are contiguous")
-        cfg.max_tokens = N = tokens.shape[1]
-        cfg.token_stride = tokens.stride(0) if B > 1 and N > 0 else N
+        cfg.max_tokens = N = shape[1]
+        cfg.token_stride = strides[0] if B > 1 and N > 0 else N
     if bias_tokens is not None or bias_values is not None:
         if (bias_tokens is None or bias_values is None or bias_tokens.dtype is not _I32 or
-                bias_values.dtype is not torch.float32 or bias_tokens.dim() != 1 or
+                bias_values.dtype is not _F32 or bias_tokens.dim() != 1 or
                 bias_tokens.shape != bias_values.shape or
                 not (bias_tokens.is_contiguous() and bias_values.is_contiguous())):
             raise ValueError("bias_tokens and bias_values must be contiguous int32 and float32 vectors of one length")
