@@ -18,15 +18,17 @@
 // floor(q_starts[b] / 16) + 2 b on, which is room enough for any position of its
 // rows, and a workgroup finds its sequence among those closed sums.
 //
-// What bounds it.  Many rows: vector instructions, busy 81 % of the time beside the
-// bytes: 8,192 rows of 32/8 heads with norms take 50 us for 185 MB (3.7 TB/s; a large
-// copy of as many takes 38).  Rotation and norm of two values are about ten of them,
-// and nothing is worked out twice.  Norm weights in one factor with the angles, and a
-// conversion that divides by the power, brought 53 to 50.  Several KV heads to a
-// workgroup, which find their sequence and angles once, take 56 (2), 64 (4) and 73 us
-// (8): fewer loads are under way.  Bounds on registers for more wavefronts: 74 and 117
-// (spills).  Few rows: the chain starts -> lengths -> rows -> maximum -> stores, 6 us
-// for 8 of them.
+// What bounds it.  Many rows: vector instructions beside the bytes: 8,192 rows of 32/8
+// heads with norms take 44.7 us for 185 MB (4.1 TB/s; a large copy of as many takes
+// 38).  From 53: norm weights in one factor with the angles, and a conversion that
+// divides by the power, 50; the order of pairs a constant of the kernel, and
+// frequencies loaded with the rows instead of one by one behind them, 48.5; no guard
+// around each row's load, and sines by a series that takes turns, 47; norm weights
+// loaded with the rows 44.7.  Several KV heads to a workgroup, which find their
+// sequence and angles once, took 56 (2), 64 (4) and 73 us (8) instead of 53: fewer
+// loads are under way.  Bounds on registers for five wavefronts per SIMD instead of
+// four: 49.2 instead of 48.5; for more: 74 and 117 (spills).  Few rows: the chain
+// starts -> lengths -> rows -> maximum -> stores, 4.6 us for 8 of them in a graph.
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"
