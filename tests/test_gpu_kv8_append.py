@@ -157,6 +157,19 @@ def test_append_skips_rows_outside_the_pool():
     check(s, False, "append a sequence without a length")
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_frequencies_at_any_element(interleaved):
+    """Frequencies that start at no multiple of 16 bytes, and end with their memory's last."""
+    import torch
+    for heads in ((12, 1, 128), (4, 2, 64)):
+        s = inputs(heads, ([1, 20, 40], [7, 0, 1000]), 48, "both", seed=9)
+        for offset in (1, 2, 3):
+            freq = torch.full((s["inv_freq"].numel() + offset,), float("nan"), device="cuda")
+            freq[offset:] = s["inv_freq"]
+            t = dict(s, inv_freq=freq[offset:])
+            check(t, interleaved, f"append {heads} frequencies {offset} elements on {interleaved}")
+
+
 def test_append_again_changes_nothing():
     """A second call with the same rows writes the same bytes: what it raised is raised."""
     import torch
