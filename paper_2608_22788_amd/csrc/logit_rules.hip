@@ -21,16 +21,21 @@
 //
 // In place, a thread that has nothing to change neither reads nor writes.
 //
-// What bounds it.  Many rows: vector instructions, busy 85 % of the time at 200 rows
-// of 151,936 bf16 logits, masks, biases and texts of 4,000 tokens on average (45 us;
-// the bytes alone need 26): 133 for a wavefront's 512 tokens of the vocabulary and
-// about as many for the text, the biases and addresses.  Slices of 8,192 tokens on
-// 1,024 threads take 47 us, on 512 threads 47, 4,096 on 256 threads 50.  Workgroups
-// that keep a row's text for several slices gain nothing (49), and working out only
-// the tokens of the text, whoever finds their count, is a longer chain (77).  Few
-// rows: the chain lengths -> tokens -> LDS -> stores (8 rows 7 us, less than the call
-// from Python).
+// What bounds it.  Many rows: vector instructions beside the bytes.  200 rows of
+// 151,936 bf16 logits, masks, biases and texts of 4,000 tokens on average take 38.5 us
+// (the bytes alone need 26): 133 instructions for a wavefront's 512 tokens of the
+// vocabulary and about as many for the text, the biases and addresses.  What mattered
+// is that no load waits for another: logits and masks stay as they are in memory until
+// the text is counted (45.6 -> 42.4), a row's numbers are loaded together (41.8), and
+// no lane's load of logits is masked off, which made the compiler wait for it to move
+// registers (38.5).  At 45 us, slices of 8,192 tokens on 1,024 threads took 47 us, on
+// 512 threads 47, 4,096 on 256 threads 50; workgroups that keep a row's text for
+// several slices 49; working out only the tokens of the text, whoever finds their
+// count, is a longer chain (77).  Few rows: the chain lengths -> tokens -> LDS ->
+// stores (8 rows 8 us in a graph, about the call from Python).
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "attn_common.h"
 #include "ts_attn.h"
@@ -51,15 +56,20 @@ constexpr uint32_t kNone = 0x80000000u;         // no bias: -0, which added chan
 struct RulesParams {
     const void *logits;
     void *out;
-    const int32_t *tokens, *lens, *prompt_lens;
+    const int32_t *tokens;
+    // A row's numbers, each an array with an entry for each row whatever is given
+    // (`has`), so that they are loaded together; all NULL if nothing of them is.
+    const int32_t *lens, *prompt_lens, *bias_starts;
     const float *repetition, *frequency, *presence;
-    const int32_t *bias_starts, *bias_tokens;
+    const int32_t *bias_tokens;
     const float *bias_values;
     const uint32_t *allowed;
     int64_t row_stride, out_stride, token_stride, allowed_stride;
     int vocab, slices, max_tokens, num_biases;
     bool in_place;
+    uint8_t has;
 };
+constexpr int kHasPrompt = 1, kHasRepetition = 2, kHasFrequency = 4, kHasPresence = 8;
 
 // Loads and stores of any element alignment.
 template <typename T, int N>
@@ -67,20 +77,39 @@ struct __attribute__((packed, aligned(sizeof(T)))) Many {
     T x[N];
 };
 
-__device__ __forceinline__ float value_of(float x) { return x; }
-__device__ __forceinline__ float value_of(uint16_t x) { return bf16_lo(x); }
-
+// A thread's eight logits as they are in memory.  Nothing is done with them until
+// load8_rest, so that the loads behind theirs do not wait for them.
 template <typename T>
-__device__ __forceinline__ void load8(const T *src, int n, float x[kPer]) {
-    if (n >= kPer) {
-        const auto v = *reinterpret_cast<const Many<T, kPer> *>(src);
+struct Raw8 {
+    uint32_t w[kPer * sizeof(T) / 4];
+    __device__ __forceinline__ float value(int e) const {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(w[e]);
+        else
+            return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+    }
+};
+template <typename T>
+__device__ __forceinline__ void load8(const T *src, int n, Raw8<T> &r) {
+    if (n >= kPer)
+        __builtin_memcpy(&r, reinterpret_cast<const Many<T, kPer> *>(src), sizeof r);
+}
+// Those of a row's last thread, if it has fewer.
+template <typename T>
+__device__ __forceinline__ void load8_rest(const T *src, int n, Raw8<T> &r) {
+    if (n <= 0 || n >= kPer)
+        return;
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
+    Bits x[kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; e++)
-            x[e] = value_of(v.x[e]);
-    } else {
+    for (int e = 0; e < kPer; e++)
+        x[e] = reinterpret_cast<const Bits *>(src)[min(e, n - 1)];
 #pragma unroll
-        for (int e = 0; e < kPer; e++)
-            x[e] = e < n ? value_of(src[e]) : 0.0f;
+    for (int i = 0; i < (int)(sizeof r / 4); i++) {
+        if constexpr (sizeof(T) == 4)
+            r.w[i] = x[i];
+        else
+            r.w[i] = (uint32_t)x[2 * i] | (uint32_t)x[2 * i + 1] << 16;
     }
 }
 __device__ __forceinline__ void store8(float *dst, int n, const float x[kPer]) {
@@ -120,10 +149,7 @@ __device__ __forceinline__ void lds_sync() {
 }
 
 // A penalty, or `off` where it is not given or not finite.
-__device__ __forceinline__ float penalty(const float *p, int b, float off) {
-    const float x = p ? __int_as_float(ld_meta(reinterpret_cast<const int32_t *>(p), b)) : off;
-    return fabsf(x) < INFINITY ? x : off;
-}
+__device__ __forceinline__ float penalty(bool given, float x, float off) { return given && fabsf(x) < INFINITY ? x : off; }
 
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
@@ -140,36 +166,38 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     // Lengths, then every first load, before anything waits for one.
     int first = 0, end = 0, len = 0, prompt = 0;
     float rep = 1.0f, freq = 0.0f, pres = 0.0f;
-    if (p.bias_tokens) {
-        first = ld_meta(p.bias_starts, b);
-        end = ld_meta(p.bias_starts, b + 1);
-    }
-    if (p.tokens) {
-        len = ld_meta(p.lens, b);
-        prompt = p.prompt_lens ? ld_meta(p.prompt_lens, b) : 0;
-        rep = penalty(p.repetition, b, 1.0f);
+    if (p.lens) {
+        const auto number = [&](const float *x) { return __int_as_float(ld_meta(reinterpret_cast<const int32_t *>(x), b)); };
+        const int bias_first = ld_meta(p.bias_starts, b), bias_end = ld_meta(p.bias_starts, p.bias_tokens ? b + 1 : b);
+        const int text_len = ld_meta(p.lens, b), prompt_len = ld_meta(p.prompt_lens, b);
+        const float r = number(p.repetition), f = number(p.frequency), q = number(p.presence);
+        first = p.bias_tokens ? bias_first : 0;
+        end = p.bias_tokens ? bias_end : 0;
+        len = p.tokens ? text_len : 0;
+        prompt = p.has & kHasPrompt ? prompt_len : 0;
+        rep = penalty(p.has & kHasRepetition, r, 1.0f);
         rep = rep > 0.0f ? rep : 1.0f;
-        freq = penalty(p.frequency, b, 0.0f);
-        pres = penalty(p.presence, b, 0.0f);
+        freq = penalty(p.has & kHasFrequency, f, 0.0f);
+        pres = penalty(p.has & kHasPresence, q, 0.0f);
     }
-    float x[kPer];
-    if (!p.in_place)
-        load8(src, n, x);
-    uint32_t closed = 0;                                      // bit e: token e is not allowed
-    if (p.allowed && n > 0) {
-        const int v = base + kPer * tid;
-        closed = ~p.allowed[b * p.allowed_stride + v / 32] >> v % 32 & ((1u << kPer) - 1);
-    }
+    // (Threads without eight logits read the row's first ones: no lane is masked.)
+    Raw8<TI> raw;
+    if (!p.in_place && p.vocab >= kPer)
+        load8(n >= kPer ? src : src - (base + kPer * tid), kPer, raw);
+    uint32_t open = ~0u;                                      // the mask's word of this thread's tokens
+    if (p.allowed && n > 0)
+        open = p.allowed[b * p.allowed_stride + (base + kPer * tid) / 32];
     first = min(max(first, 0), p.num_biases);
     end = min(max(end, 0), p.num_biases);
     len = min(max(len, 0), p.max_tokens);
     prompt = min(max(prompt, 0), len);
-    uint32_t bias_at = ~0u;                                   // place in the slice of the bias that this thread holds
+    int32_t bias_token = 0;                                   // the bias that this thread holds, if there is one
     float bias_w = 0.0f;
     const auto load_bias = [&](int j0) {
-        const int j = j0 + tid;
-        bias_at = j < end ? (uint32_t)p.bias_tokens[j] - (uint32_t)base : ~0u;
-        bias_w = j < end ? p.bias_values[j] : 0.0f;
+        if (j0 + tid < end) {
+            bias_token = p.bias_tokens[j0 + tid];
+            bias_w = p.bias_values[j0 + tid];
+        }
     };
     if (first < end)
         load_bias(first);
@@ -189,7 +217,11 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
         }
     };
     load_text(0);
-    const int32_t odd = whole + tid < len ? text[whole + tid] : -1;   // the last tokens
+    int32_t odd = -1;                                         // the last tokens
+    if (whole + tid < len)
+        odd = text[whole + tid];
+    if (!p.in_place)
+        load8_rest(src, n, raw);
 
     u32x4_t *const zero = reinterpret_cast<u32x4_t *>(lds);
 #pragma unroll
@@ -201,7 +233,8 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     lds_sync();
 
     for (int j0 = first; j0 < end; j0 += kThreads) {
-        bool pending = bias_at < here;
+        const uint32_t bias_at = (uint32_t)bias_token - (uint32_t)base;   // its place in the slice
+        bool pending = j0 + tid < end && bias_at < here;
         const uint32_t mine = kThreads - tid;             // the first thread has the largest
         for (;;) {
             if (tid == 0)
@@ -267,6 +300,8 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
         return;
     uint32_t c[kPer];
     float w[kPer];
+    asm volatile("" : "+v"(open));                            // (or it would be turned round where it is loaded, and waited for)
+    const uint32_t closed = ~open >> (base + kPer * tid) % 32 & ((1u << kPer) - 1);   // bit e: token e is not allowed
     bool any = closed != 0;
 #pragma unroll
     for (int e = 0; e < kPer; e += 4) {
@@ -284,12 +319,15 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     if (p.in_place) {
         if (!any)
             return;
-        load8(src, n, x);
+        load8(src, n, raw);
+        load8_rest(src, n, raw);
     }
     // (Without branches, which some token of a wavefront's 512 would mostly take.)
     const float inverse = 1.0f / rep;
+    float x[kPer];
 #pragma unroll
     for (int e = 0; e < kPer; e++) {
+        x[e] = raw.value(e);
         const uint32_t times = c[e] & ~kInPrompt;
         x[e] *= c[e] ? x[e] > 0.0f ? inverse : rep : 1.0f;
         x[e] -= times ? freq * (float)times + pres : 0.0f;
@@ -355,13 +393,17 @@ int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, co
     p.logits = logits;
     p.out = out;
     p.tokens = penalties && cfg->max_tokens > 0 ? tokens : nullptr;
-    p.lens = lens;
-    p.prompt_lens = prompt_lens;
-    p.repetition = repetition;
-    p.frequency = frequency;
-    p.presence = presence;
-    p.bias_starts = bias_starts;
     p.bias_tokens = bias_starts && cfg->num_biases > 0 ? bias_tokens : nullptr;
+    const int32_t *const some = p.tokens ? lens : p.bias_tokens ? bias_starts : nullptr;
+    p.lens = p.tokens ? lens : some;
+    p.prompt_lens = p.tokens && prompt_lens ? prompt_lens : some;
+    p.bias_starts = p.bias_tokens ? bias_starts : some;
+    const auto given = [&](const float *x) { return p.tokens && x ? x : reinterpret_cast<const float *>(some); };
+    p.repetition = given(repetition);
+    p.frequency = given(frequency);
+    p.presence = given(presence);
+    p.has = (prompt_lens ? kHasPrompt : 0) | (repetition ? kHasRepetition : 0) | (frequency ? kHasFrequency : 0) |
+            (presence ? kHasPresence : 0);
     p.bias_values = bias_values;
     p.allowed = allowed;
     p.row_stride = cfg->row_stride;
