@@ -492,8 +492,9 @@ int ts_chunk_attn_kv8(const ts_chunk_shape *shape, const void *q, int64_t q_stri
  *   allowed      uint32 [num_seqs][vocab / 32, rounded up], rows allowed_stride words
  *                apart: token v is allowed if bit v % 32 of word v / 32 is set
  * Without tokens, without all three bias arrays, without allowed (NULL) that rule is
- * off.  Asynchronous on `stream`, one launch, no workspace; results do not depend
- * on any order but the lists'. */
+ * off.  Asynchronous on `stream`, no workspace, one launch (two or three where
+ * num_seqs x ceil(vocab / 4096) is 2^23 or more); results do not depend on any
+ * order but the lists'. */
 #define TS_LOGITS_F32 0
 #define TS_LOGITS_BF16 1
 

@@ -17,7 +17,8 @@
 // threads that hold biases of one token, the first adds its own, then the next
 // (three barriers for each, so a list that names one token over and over takes time
 // for every mention).
-// One launch, nothing kept in memory between slices or calls.
+// One launch (of shapes with 2^23 slices and more, another for the rows behind those
+// that fill one), nothing kept in memory between slices or calls.
 //
 // In place, a thread that has nothing to change neither reads nor writes.
 //
@@ -35,6 +36,7 @@
 // stores (8 rows 8 us in a graph, about the call from Python).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.h"
@@ -46,6 +48,7 @@ namespace tsattn {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kMostGroups = (1 << 23) - 1;     // of a launch, which has less than 2^32 threads
 constexpr int kPer = 8;                        // tokens of a thread
 constexpr int kSlice = kThreads * kPer;
 constexpr int kAhead = 4;                      // groups of four text tokens whose loads are in flight together
@@ -65,7 +68,7 @@ struct RulesParams {
     const float *bias_values;
     const uint32_t *allowed;
     int64_t row_stride, out_stride, token_stride, allowed_stride;
-    int vocab, slices, max_tokens, num_biases;
+    int first_row, vocab, slices, max_tokens, num_biases;
     bool in_place;
     uint8_t has;
 };
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void logit_rules_kernel(RulesParams p) {
     float *const bias = reinterpret_cast<float *>(lds + kTable);   // [kSlice], where there are biases
     __shared__ int s_pending;
     const int at = xcd_worker(blockIdx.x, gridDim.x);
-    const int b = at / p.slices, base = at % p.slices * kSlice, tid = threadIdx.x;
+    const int b = p.first_row + at / p.slices, base = at % p.slices * kSlice, tid = threadIdx.x;
     const int n = p.vocab - base - kPer * tid;                // of this thread's tokens exist
     const TI *const src = static_cast<const TI *>(p.logits) + b * p.row_stride + base + kPer * tid;
     TO *const dst = static_cast<TO *>(p.out) + b * p.out_stride + base + kPer * tid;
@@ -418,10 +421,16 @@ int ts_logit_rules(const ts_rules_config *cfg, const void *logits, void *out, co
     const bool f_in = cfg->logits_type == TS_LOGITS_F32, f_out = cfg->out_type == TS_LOGITS_F32;
     const auto kernel = f_in ? f_out ? logit_rules_kernel<float, float> : logit_rules_kernel<float, uint16_t>
                              : f_out ? logit_rules_kernel<uint16_t, float> : logit_rules_kernel<uint16_t, uint16_t>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(cfg->num_seqs * p.slices)), dim3(kThreads),
-                       (kTable + (p.bias_tokens ? kSlice : 0)) * sizeof(uint32_t), reinterpret_cast<hipStream_t>(stream), p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? TS_OK : hip_fail(e, "logit rules launch");
+    const size_t lds = (kTable + (p.bias_tokens ? kSlice : 0)) * sizeof(uint32_t);
+    const int row_step = kMostGroups / p.slices;   // rows of a launch
+    for (p.first_row = 0; p.first_row < cfg->num_seqs; p.first_row += row_step) {
+        const int rows = std::min(row_step, cfg->num_seqs - p.first_row);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * p.slices)), dim3(kThreads), lds, reinterpret_cast<hipStream_t>(stream), p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return hip_fail(e, "logit rules launch");
+    }
+    return TS_OK;
 }
 
 }  // extern "C"

@@ -187,3 +187,24 @@ def test_rules_copies_what_no_rule_names(types):
         want, got = x.to(bf[types[1]])[:, :5002].contiguous(), out[:, :5002].contiguous()
         bits = torch.int32 if types[1] == "f" else torch.int16
         assert torch.equal(got.view(bits), want.view(bits)), kw.keys()
+
+
+def test_rules_on_more_workgroups_than_one_launch_has():
+    """65,536 rows of 520,193 tokens in place (68 GB): 2^23 workgroups.  Every row
+    has a bias for its last token and for one of its own; every logit is compared."""
+    import torch
+    from paper_2608_22788_amd import binding
+    B, V = 65536, 127 * 4096 + 1
+    say("rules on 65,536 rows of 520,193 tokens")
+    x = torch.zeros(B, V, dtype=torch.bfloat16, device="cuda")
+    row = torch.arange(B, device="cuda")
+    own = row * 7919 % (V - 1)
+    w = (1 + row % 7).float()
+    binding.logit_rules(x, x, bias_starts=torch.arange(0, 2 * B + 1, 2, dtype=torch.int32, device="cuda"),
+                        bias_tokens=torch.stack((own, torch.full_like(own, V - 1)), 1).flatten().to(torch.int32),
+                        bias_values=torch.stack((w, -w), 1).flatten())
+    for at, want in ((own, w), (torch.full_like(own, V - 1), -w)):
+        assert torch.equal(x[row, at].float(), want)
+        x[row, at] = 0.0
+    for part in x.view(torch.int16).split(4096):
+        assert int(part.count_nonzero()) == 0, "a token that no rule names was changed"
