@@ -21,6 +21,7 @@
  *     query head h reads KV head h / (Hq / Hkv)  (contiguous GQA groups);
  *     K_t = k_pages[page_table[b][t / P]][g][t % P][:], V_t likewise;
  *     out[b][i][h][:] = sum_t softmax_t(scale * <q[b][i][h][:], K_t>) V_t.
+ * A row that sees a NaN key, or whose query holds one, is NaN.
  *
  * Memory layouts (row-major, all device memory unless stated):
  *   q, out      bf16  [num_seqs][max_q_len][num_q_heads][head_dim]

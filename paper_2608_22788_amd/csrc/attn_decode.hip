@@ -278,7 +278,7 @@ struct DecodeQ1 {
                 } else {
                     const size_t row = (size_t)slot_id * p.rows_per_unit + r;
                     float *dst = p.ws_o + row * D;
-                    const float lse = l > 0.0f ? M + __log2f(l) : -INFINITY;
+                    const float lse = piece_lse(M, l);
                     if (p.combine != kCombineKernel) {
                         // device-coherent stores: another wavefront of this
                         // launch combines them

@@ -75,6 +75,13 @@ __device__ __forceinline__ void wait_vmem() {
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
+// log2-sum-exp of a piece with sum l relative to 2^m, -inf for one without a
+// visible key, which the join passes over.  A sum that is NaN (a NaN score) has a
+// finite one, so that the piece's values, all NaN, are taken along.
+__device__ __forceinline__ float piece_lse(float m, float l) {
+    return l > 0.0f ? m + __log2f(l) : l == 0.0f ? -INFINITY : 0.0f;
+}
+
 // Running log-sum-exp combination of partials for one lane's VE dims.
 template <int VE>
 struct Acc {

@@ -426,13 +426,6 @@ struct Verify {
         }
     }
 
-    // log2-sum-exp of a piece with sum l relative to 2^m.  A sum that is NaN (a NaN
-    // score) has a finite one, so that the join, which passes over pieces without a
-    // key (-inf), takes the piece's NaN values along.
-    __device__ __forceinline__ static float partial_lse(float m, float l) {
-        return l > 0.0f ? m + __log2f(l) : k8 && l != 0.0f ? 0.0f : -INFINITY;
-    }
-
     // A piece of a split unit as one wavefront of a group leaves it in LDS:
     // the sums of P V relative to 2^m in the wavefront's own lane order (so
     // that writes and reads are free of bank conflicts), and where they go.
@@ -527,7 +520,7 @@ struct Verify {
                 } else if constexpr (!kGroup) {
                     const size_t row = (size_t)slot_id * R + r;
                     float *dst = p.ws_o + row * D + VE * n;
-                    const float lse = partial_lse(m, l);
+                    const float lse = piece_lse(m, l);
                     if (p.combine != kCombineKernel) {
                         // device-coherent: another wavefront of this launch combines them
 #pragma unroll
@@ -747,7 +740,7 @@ struct Verify {
                         *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
                     continue;
                 }
-                const float lse = partial_lse(M, a.den);
+                const float lse = piece_lse(M, a.den);
                 const size_t row = (size_t)slot * R + r;
 #pragma unroll
                 for (int e = 0; e < VE; e += 4) {

@@ -409,7 +409,7 @@ struct Team {
                     dst[16 * jj] = to_bf16(st.acc[jj][i] * inv);
             } else {
                 const size_t row = (size_t)slot_id * R + r;
-                const float lse = l > 0.0f ? M[i] + __log2f(l) : -INFINITY;
+                const float lse = piece_lse(M[i], l);
                 if (p.combine != kCombineKernel) {
                     // device-coherent: merge workgroups of this launch read them
 #pragma unroll
