@@ -412,8 +412,10 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *                     one for the values of each page and KV head
  * A cached value is code * 2^(byte - 127), exactly a bf16 number for the bytes 27
  * to 227 that ts_rope_append_kv8 writes (the powers 2^-100 to 2^100); with others
- * from 1 to 254 the product is taken as bf16 takes it; 0 and 255 are not for pages
- * that hold tokens.  Code 0x7f (and 0xff) is NaN; e4m3 has no
+ * from 1 to 246 the product is taken as bf16 takes it, and finite.  0 and 247 to
+ * 255 are not for pages that hold tokens: a code times such a power may be infinite,
+ * also one that a row does not see or that lies behind the last token, and its
+ * weight of zero would make the row NaN.  Code 0x7f (and 0xff) is NaN; e4m3 has no
  * infinity. */
 
 /* ts_rope_append into the cache held in 8 bits.  Norm and rotation in float32 as

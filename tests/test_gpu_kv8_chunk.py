@@ -6,7 +6,7 @@ import pytest
 
 from gpu_util import say
 from test_gpu_chunk import CANARY, SHAPES, f64, make
-from test_gpu_kv8_decode import NAN, eight_bits, reference8, within
+from test_gpu_kv8_decode import NAN, eight_bits, largest_power, reference8, within
 
 pytestmark = pytest.mark.gpu
 
@@ -204,3 +204,19 @@ def test_pages_behind_4_gib():
         s[name] = far
     s["table"] = torch.where(table >= 0, place[table.clamp(min=0)], table).to(torch.int32).contiguous()
     check(s, "chunk8 far pages", ref)
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (16, 1, 128), (8, 2, 64)], ids=str)
+def test_the_largest_power(heads):
+    """As in test_gpu_kv8_decode.py: in row tiles of few rows and of many."""
+    q = [1, 5, 70, 3]
+    s = make8(heads, q, [99, 700, 26, 0], seed=12)
+    largest_power(s, [n - min(k, 3) + 1 for n, k in zip(s["ctx"].tolist(), q)])   # the last one or two rows see some
+    want, mag = reference(s)
+    ends = np.cumsum(q)
+    keep = np.ones(int(ends[-1]), dtype=bool)
+    for e, n in zip(ends, q):
+        keep[e - min(n, 3) + 1:e] = False
+    for workers in (0, 1, 5, 64):
+        say("chunk8 largest power", heads, workers)
+        within(f64(run(s, num_workers=workers))[keep], want[keep], mag[keep], f"chunk8 largest power {heads}")

@@ -192,3 +192,36 @@ def test_pages_behind_4_gib():
     ref = decode_reference(near)
     s["scales"], s["table"] = scales, torch.where(table >= 0, place[table.clamp(min=0)], table).to(torch.int32).contiguous()
     check_decode(s, "kv8 far pages", ref)
+
+
+def largest_power(s, seen_by_all, byte=246):
+    """The last page of every sequence at the largest power that a cache may have:
+    codes of zero for the tokens that all rows see (`seen_by_all` of each sequence),
+    +-448 for the others and for the slots behind the last token."""
+    import torch
+    for b, n in enumerate(s["ctx"].tolist()):
+        pid = int(s["table"][b, (n - 1) // 16])
+        s["scales"].view(torch.uint8)[pid] = byte
+        for k, name in enumerate(("k_pages", "v_pages")):
+            codes = s[name].view(torch.uint8)[pid]
+            codes[:] = 0
+            first = max(seen_by_all[b] - (n - 1) // 16 * 16, 0)
+            codes[:, first:, ::2], codes[:, first:, 1::2] = (0x7e, 0xfe) if k else (0xfe, 0x7e)
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (64, 4, 128), (8, 2, 64), (16, 1, 64)], ids=str)
+@pytest.mark.parametrize("qmax", [1, 4])
+def test_the_largest_power(heads, qmax):
+    """Rows that do not see values of 448 times the largest power, the largest finite
+    ones of bf16, are as without them."""
+    s = make8(heads, [qmax, qmax, 1], [100, 20 + qmax, 900], seed=11, qmax=qmax)
+    largest_power(s, [n - q + 1 for n, q in zip(s["ctx"].tolist(), s["ql"].tolist())])
+    from paper_2608_22788_amd import binding
+    import torch
+    want, mag = decode_reference(s)
+    first = np.concatenate(([0], np.cumsum(s["ql"].cpu().numpy())))[:-1]   # the rows that see none
+    for workers in (0, 1, 3, 50):
+        out = torch.zeros_like(s["q4"])
+        binding.decode_attn_kv8(s["q4"], s["k_pages"], s["v_pages"], s["scales"], s["table"], s["ctx"], s["ql"], out,
+                                s["scale"], max_ctx_len=s["max_ctx"], num_workers=workers)
+        within(f64(out)[:, 0], want[first], mag[first], f"kv8 largest power {heads} workers {workers}")
