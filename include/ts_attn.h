@@ -428,8 +428,12 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  *   same value, but where it falls below 2^(k - 6) (e4m3's denormal range);
  *   code = e4m3(x / 2^k), nearest even.
  * Powers stay inside 2^-100 .. 2^100 and larger values are held as +-448 * 2^100.
- * Infinite and NaN values are held as NaN and do not count for m.  The bytes that
- * a page held behind its last token are not looked at, and kept.  Two sequences
+ * Infinite and NaN values are held as NaN and do not count for m.  A page's power
+ * never falls while it holds a token in front of the new ones: if tokens are taken
+ * back (rejected drafts, with ctx_lens set back to the accepted ones) and others
+ * appended in their place, the power that they raised stays, and so does what the
+ * codes in front lost to it, until the page is appended to from its first slot on.
+ * The bytes that a page held behind its last token are not looked at, and kept.  Two sequences
  * must not append to one page in one call, as they must not to one slot of the
  * bf16 cache.  Otherwise arguments, limits and errors are those of
  * ts_rope_append. */

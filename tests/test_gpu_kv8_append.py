@@ -180,3 +180,38 @@ def test_append_again_changes_nothing():
     run(s, False, out)
     for a, n in zip(first, ("k_pages", "v_pages", "scales")):
         assert (a == u8(s[n])).all(), n
+
+
+@pytest.mark.parametrize("rejected", [1, 3])
+def test_append_behind_rejected_drafts(rejected):
+    """A draft block whose last row is large, of which the last `rejected` rows are taken
+    back, and rows in their place: the page keeps the power that they raised, and the
+    accepted tokens one rounding more, until it is filled from its first slot on."""
+    import torch
+    first = inputs((4, 2, 64), ([6], [0]), 0, "none", seed=10)
+    cache = {n: first[n] for n in ("k_pages", "v_pages", "scales", "table")}
+    said = {"k": [], "v": []}
+
+    def step(tokens, past, tag, big=None):
+        s = dict(inputs((4, 2, 64), ([tokens], [past]), 0, "none", seed=11 + past), **cache)
+        if big is not None:
+            for n in said:
+                s[n][tokens - 1] *= big            # (rows behind belong to no sequence)
+        check(s, False, tag)
+        for n in said:
+            said[n] = said[n][:past] + list(f64(s[n])[:tokens])
+
+    step(6, 0, "accepted tokens")
+    step(4, 6, "a draft block", big=2.0 ** 12)
+    raised = u8(cache["scales"])[int(cache["table"][0, 0])].copy()
+    step(3, 10 - rejected, "behind rejected drafts")
+    pid = int(cache["table"][0, 0])
+    assert (u8(cache["scales"])[pid] == raised).all(), "the page's power after drafts were taken back"
+    for which, (n, pages) in enumerate((("k", "k_pages"), ("v", "v_pages"))):
+        power = np.exp2(raised[:, which] - 127.0)[:, None, None]
+        held = kv8.code_values()[u8(cache[pages])[pid]] * power
+        x = np.stack(said[n], 1)                                   # [heads][tokens][D], exact (no norm, no rotation)
+        err = np.abs(held[:, :x.shape[1]] - x)
+        assert (err <= 2.0 ** -4 * np.abs(x) + 2 * 2.0 ** -10 * power).all(), f"{n}: two roundings"
+    step(2, 0, "the page from its first slot on")
+    assert (u8(cache["scales"])[pid] < raised).all()
