@@ -8,7 +8,9 @@
 // along (one instruction for two values); and when a later token raises a page's
 // power, the codes that the page holds already only move their exponents, so a
 // value is rounded once (again only below 2^-6 of the power, where e4m3 is
-// denormal).  It costs nothing in precision: e4m3's steps are relative.
+// denormal).  A rounding is off by at most max(2^-4 of the value, 2^-10 of the
+// power): values below 2^-10 of their page's power, beside one that is far larger,
+// become zero.
 #pragma once
 
 #include "attn_common.h"

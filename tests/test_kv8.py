@@ -155,6 +155,28 @@ def test_oracle_power(amax, byte):
     assert amax <= 448.0 * 2.0 ** (byte - 127) or byte == 227
 
 
+def test_oracle_one_large_value_in_a_page():
+    """What a page's one power costs: a value is off by at most half a step, 2^-4 of
+    itself, but never less than 2^-10 of the power; below that it is lost."""
+    rng = np.random.default_rng(3)
+    heads, D = 1, 64
+    k = rng.normal(size=(16, heads, D))
+    k[5, 0, 7] = 448.0 * 2.0 ** 6
+    codes, bytes_ = np.zeros((1, heads, 16, D), dtype=np.uint8), np.full((1, heads, 2), 127, dtype=np.uint8)
+    _, want, _, after = kv8.append(k, k, k, codes, codes, bytes_, np.zeros((1, 1), dtype=int), [16], [0, 16], np.zeros(0))
+    assert after[0, 0, 0] == 127 + 6
+    grid = kv8.code_values()[:127]                                 # 0 .. 448, ascending
+    size = np.abs(want[0, 0])
+    held = np.sign(want[0, 0]) * grid[np.abs(size[..., None] - grid).argmin(-1)] * 2.0 ** 6
+    x = k[:, 0]
+    assert (np.abs(held - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * 2.0 ** 6)).all()
+    assert (np.abs(held - x) <= kv8.half_step(size) * 2.0 ** 6).all()
+    small = np.abs(x) < 2.0 ** -10 * 2.0 ** 6
+    assert small.sum() > 20 and (held[small] == 0).all()           # lost whole
+    middle = ~small & (np.abs(x) < 2.0 ** -6 * 2.0 ** 6)           # denormal codes
+    assert (np.abs(held - x)[middle] > 2.0 ** -4 * np.abs(x)[middle]).any()
+
+
 def test_every_call_hands_its_stream_and_tensors_to_the_device_check(monkeypatch):
     seen = []
 
