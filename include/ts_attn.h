@@ -483,8 +483,10 @@ int ts_chunk_attn_kv8(const ts_chunk_shape *shape, const void *q, int64_t q_stri
  *                row_stride / out_stride elements apart (at least vocab, any
  *                alignment of an element); out may be logits itself, with one type
  *                and stride, and must not overlap them otherwise; num_seqs 1 ..
- *                65536, vocab 1 .. 2^20.  In place, only what the rules change is
- *                read or written.
+ *                65536, vocab 1 .. 2^20.  In place, eight neighbouring tokens 8 i ..
+ *                8 i + 7 of a row none of which is in its text, biased or not
+ *                allowed are neither read nor written; others may be read and
+ *                rewritten whole, so nothing else may write to the row meanwhile.
  *   tokens       int32 [num_seqs][max_tokens], rows token_stride apart: each row's
  *                text, prompt first; ids outside [0, vocab) count nowhere
  *   lens, prompt_lens  int32 [num_seqs], clamped to [0, max_tokens] and [0, lens];

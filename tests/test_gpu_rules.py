@@ -208,3 +208,36 @@ def test_rules_on_more_workgroups_than_one_launch_has():
         x[row, at] = 0.0
     for part in x.view(torch.int16).split(4096):
         assert int(part.count_nonzero()) == 0, "a token that no rule names was changed"
+
+
+@pytest.mark.parametrize("dtype", ["f", "b"])
+def test_rules_in_place_leave_groups_that_no_rule_names(dtype):
+    """Eight neighbouring tokens without a named one keep their bits, signalling NaNs'
+    too, which arithmetic would make quiet; a named token's neighbours keep their
+    values."""
+    import torch
+    from paper_2608_22788_amd import binding
+    V, kind, bits, snan = 5003, *((torch.float32, torch.int32, 0x7f800001) if dtype == "f" else
+                                  (torch.bfloat16, torch.int16, 0x7f81))
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    x = torch.randn(3, V, device="cuda").to(kind)
+    raw = x.view(bits)
+    raw[:, ::5] = snan
+    for text, biases in (([16, 4099], [(1, 2500), (2, 5002)]), ([0], [])):
+        named = torch.zeros(3, V, dtype=torch.bool, device="cuda")
+        named[:, text] = True
+        for b, t in biases:
+            named[b, t] = True
+        group = torch.nn.functional.pad(named, (0, -V % 8)).view(3, -1, 8).any(2).repeat_interleave(8, 1)[:, :V]
+        before = raw.clone()
+        kw = {}
+        if biases:
+            kw = dict(bias_starts=i32([0, 0, 1, 2]), bias_tokens=i32([t for _, t in biases]),
+                      bias_values=torch.full((2,), 3.0, device="cuda"))
+        binding.logit_rules(x, x, tokens=i32([text] * 3), lens=i32([len(text)] * 3),
+                            presence=torch.full((3,), 0.5, device="cuda"), **kw)
+        assert torch.equal(raw[~group], before[~group])
+        beside = group & ~named
+        assert torch.equal(torch.nan_to_num(x[beside].float()), torch.nan_to_num(before.view(kind)[beside].float()))
+        odd = before.view(kind).isnan()
+        assert torch.equal(x.isnan(), odd) and (raw != before)[named & ~odd].all()
