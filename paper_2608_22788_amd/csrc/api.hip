@@ -95,9 +95,10 @@ struct Plan {
 // would allow 3: the third team lowers throughput by 8 %.  The auto count is further capped at launch by
 // the occupancy the HIP runtime reports for the compiled kernel, so all
 // workers run in one round.
-// A cache in 8 bits with three and more row blocks keeps the vector units busy rather
-// than memory: 4 there too (4 sequences of 32-98 thousand tokens, 64 rows: 148 against
-// 178 us with 3; 64 of 500-8,000: 178 against 216).
+// A cache in 8 bits with three and more row blocks: a wavefront has a SIMD's registers
+// to itself and takes longer over a page than memory does, so 3 leave a SIMD idle; 4
+// there too (calls, 64 rows: 4 sequences of 32-98 thousand tokens 146 against 175 us
+// with 3, 64 of 500-8,000 tokens 175 against 213; 48 rows: 119 against 141).
 static int per_cu_bound(bool q1, bool team, int rows, bool kv8 = false) {
     if (q1)
         return 4;

@@ -74,7 +74,10 @@ struct Verify {
     static constexpr int KS = D / 32;   // k-steps of the score product
     static constexpr int VE = D / 16;   // value dims per lane = P.V products per row block
     static constexpr int kBlockBytes = kPage * D * (k8 ? 1 : 2);   // one (page, KV head) block
-    // Pages of a step: two of codes, but where the sums leave registers for one.
+    // Pages of a step: two of codes, but where the sums leave registers for one (of
+    // head_dim 128, two with three row blocks take all 512 registers and 25 in scratch:
+    // 48 rows, 4 sequences of 32-98 thousand tokens, 130 us, with one 119; with four row
+    // blocks the compiler fails).
     static constexpr int kStep = k8 && (D == 64 || NB <= 2) ? 2 : 1;
 
     struct Bf16Regs {

@@ -19,9 +19,15 @@
 // Two steps under way instead of one: no difference (346 against 348 us).
 // One sequence of 1,600: 10 us, the chain of the launch and the join of its pieces;
 // two pages per wavefront instead of four take 11.3 (more pieces).
-// 33 rows and more (64 rows, 4 sequences of 32-98 thousand tokens, 171 us, 2.95 TB/s):
-// vector instructions, as each row block has its own scores and weights.  The chunk
-// kernel takes 189 us for it, four wavefronts that share the rows of one page 296.
+// 33 rows and more (64 rows, 4 sequences of 32-98 thousand tokens, 146 us, 3.48 TB/s;
+// 48 rows 119, 4.26): the chain of the one wavefront that a SIMD's registers hold, of
+// whose time vector instructions take 36 %, matrix products 34 % and waits 25 %, one
+// after the other.  17 to 32 rows (the same sequences, 32 rows, 95 us, 5.3 TB/s; memory
+// alone 74) the same way: 47, 17 and 24 %.  When 64 rows took 186 us, the chunk kernel
+// took 189 for them, four wavefronts that share the rows of one page 296.
+// head_dim 64: 256 sequences of 500-8,000 tokens 59 us (4.9 TB/s; half of the bytes for a
+// step's work), 32 of 16-65 thousand with 64 rows 137 (2.7; vector 53 %, matrix 17 %,
+// waits 22 %).
 #include "attn_verify.h"
 
 namespace tsattn {

@@ -68,7 +68,12 @@
 // that long.  Their wavefronts share the keys instead (few_rows): 0.66 us, 6.3 TB/s
 // over the chip.  32 mixed sequences, 138 MB: 83 us without, 77 with the places of the
 // bf16 cache, 63 with those that the times of either kind ask for (chunk_partition.h).
-// Three steps under way for a wavefront instead of two spill registers: 79 us.
+// The kernel of head_dim 128 keeps 8 registers in scratch for it (36 bytes a lane; two
+// reloads are in the loop over these row tiles' keys); with three steps under way for
+// a wavefront instead of two it would be 20, and 79 us.  A piece starts cold, so
+// contexts of a few tiles gain nothing from their half of the bytes: 160 sequences
+// of one token behind 64 take 32 us (26-27 from the bf16 cache), behind 128 both 35,
+// behind 256 43 against 50, behind 4,096 247 against 406.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -741,15 +746,10 @@ struct Chunk {
         return pages;
     }
 
-    // A worker's range.  A row's query is read by the workers of its row tile
-    // alone, and output is written after it: by the one that has the whole tile,
-    // or by the merge kernel (so the output may take the queries' place).
-    // While a piece's result is written, the first tiles of
-    // the next one are already on their way.
     // ---- row tiles of up to 16 rows, of the cache held in 8 bits ------------------
     // One wavefront has rows then, so the wavefronts take turns at the keys instead:
     // wavefront w the pages 2 w, 2 w + 1 of every 16, in the steps of attn_verify.h,
-    // straight to registers, two steps ahead.  Their sums meet in LDS.
+    // straight to registers, one step ahead.  Their sums meet in LDS.
     typedef Verify<D, 1, true> Few;
     __device__ __forceinline__ static bool is_few(const ChunkParams &p, const Piece &pc) {
         const SeqInfo sq = seq_info<k8>(p, pc.b);
@@ -893,6 +893,11 @@ struct Chunk {
         lds_barrier();
     }
 
+    // A worker's range.  A row's query is read by the workers of its row tile
+    // alone, and output is written after it: by the one that has the whole tile,
+    // or by the merge kernel (so the output may take the queries' place).
+    // While a piece's result is written, the first tiles of the next one are already on
+    // their way (few_rows starts and ends by itself).
     __device__ __forceinline__ static void work(const ChunkParams &p, const uint64_t *s_end, int w, int64_t begin, int64_t end, char *lds) {
         const int lane = threadIdx.x & (kWave - 1);
         const int wave = first_lane_int(threadIdx.x / kWave);

@@ -30,11 +30,13 @@
 // is that no load waits for another: logits and masks stay as they are in memory until
 // the text is counted (45.6 -> 42.4), a row's numbers are loaded together (41.8), and
 // no lane's load of logits is masked off, which made the compiler wait for it to move
-// registers (38.5).  At 45 us, slices of 8,192 tokens on 1,024 threads took 47 us, on
-// 512 threads 47, 4,096 on 256 threads 50; workgroups that keep a row's text for
-// several slices 49; working out only the tokens of the text, whoever finds their
-// count, is a longer chain (77).  Few rows: the chain lengths -> tokens -> LDS ->
-// stores (8 rows 8 us in a graph, about the call from Python).
+// registers (38.5).  Before these, when it took 45 us, slices of 8,192 tokens on 1,024
+// threads took 47 us, on 512 threads 47, 4,096 on 256 threads 50; workgroups that keep
+// a row's text for several slices 49; working out only the tokens of the text, whoever
+// finds their count, is a longer chain (77); none was measured again since.  In place,
+// with masks on two rows of three, it takes as long (43 against 42 us in one loop).  Few
+// rows: the chain lengths -> tokens -> LDS -> stores (8 rows 8 us in a graph, about the
+// call from Python).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
