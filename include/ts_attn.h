@@ -433,9 +433,9 @@ int ts_chunk_attn(const ts_chunk_shape *shape, const void *q, int64_t q_stride, 
  * back (rejected drafts, with ctx_lens set back to the accepted ones) and others
  * appended in their place, the power that they raised stays, and so does what the
  * codes in front lost to it, until the page is appended to from its first slot on.
- * The bytes that a page held behind its last token are not looked at, and kept.  Two sequences
- * must not append to one page in one call, as they must not to one slot of the
- * bf16 cache.  Otherwise arguments, limits and errors are those of
+ * The bytes that a page held behind its last token are not looked at, and kept.
+ * Two sequences must not append to one page in one call, as they must not to one
+ * slot of the bf16 cache.  Otherwise arguments, limits and errors are those of
  * ts_rope_append. */
 int ts_rope_append_kv8(const ts_chunk_shape *shape, const ts_rope_config *cfg, const void *q, const void *k,
                        const void *v, void *q_out, void *k_pages, void *v_pages, void *kv_scales,

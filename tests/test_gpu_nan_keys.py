@@ -64,3 +64,18 @@ def test_nan_keys(case):
     for variant in variants:
         for workers in (0, 1, 5, 64):
             check(s, ref, f"NaN keys {name}", variant, workers)
+
+
+@pytest.mark.parametrize("case", [c for c in CASES if c[0] in ("short_long", "merge_kernel", "last", "d64_3")] + [ROWS64],
+                         ids=lambda c: c[0])
+def test_nan_queries(case):
+    name, Hq, Hkv, D, qmax, ql, cl, _ = case
+    s = inputs((Hq, Hkv, D), ql, [max(n, q) for n, q in zip(cl, ql)], qmax, seed=18)
+    for b, q in enumerate(ql):
+        if q > 0:
+            s["q4"][b, q - 1, (3 * b) % Hq, (7 * b) % D] = float("nan")
+    ref = reference(s)
+    assert np.isnan(ref[0]).any() and not np.isnan(ref[0]).all()
+    for variant in [0, 1] + ([TEAM] if D == 128 else []) + ([VALU] if qmax == 1 else []):
+        for workers in (0, 5):
+            check(s, ref, f"NaN queries {name}", variant, workers)

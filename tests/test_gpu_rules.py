@@ -241,3 +241,10 @@ def test_rules_in_place_leave_groups_that_no_rule_names(dtype):
         assert torch.equal(torch.nan_to_num(x[beside].float()), torch.nan_to_num(before.view(kind)[beside].float()))
         odd = before.view(kind).isnan()
         assert torch.equal(x.isnan(), odd) and (raw != before)[named & ~odd].all()
+
+
+@pytest.mark.parametrize("dtype", ["f", "b"])
+@pytest.mark.parametrize("V", [1, 7, 8, 9, 33, 4095, 4097, 12289])
+def test_rules_in_place_sizes(dtype, V):
+    for pad in (0, 3):
+        check(make(5, V, dtype, biases=9, masked=True, seed=V + pad, pad=pad, in_place=True), f"rules in place {V} pad {pad}")
