@@ -59,18 +59,20 @@
 // instruction that takes the page's power along (exact), and two stages suffice.
 // Half of the bytes, and for each value half a conversion and an eighth of an LDS
 // store, 6 % of the time in bank conflicts.  A prompt of 8,192 tokens takes 546-565 us,
-// 973-1,007 TFLOP/s (538-563 from the bf16 cache on the same boxes), 16 ragged prompts
-// of up to 1,024 tokens 312-315 us.  What mattered, on the prompt: conversions by all wavefronts at the start of a step 585
-// us; the keys' wavefronts before and the values' after it 558; ids and powers of 64
-// tiles in a lane each 548.
+// 973-1,007 TFLOP/s (538-563 from the bf16 cache on the same boxes; on another 553
+// against 521), 16 ragged prompts of up to 1,024 tokens 308-315 us.  What mattered, on
+// the prompt: conversions by all wavefronts at the start of a step 585 us; the keys'
+// wavefronts before and the values' after it 558; ids and powers of 64 tiles in a lane
+// each 548.
 // Row tiles of up to 16 rows (decoding sequences) would have one busy wavefront of
 // eight and take 1.2 us a KV tile, as long as from the bf16 cache, whose bytes take
 // that long.  Their wavefronts share the keys instead (few_rows): 0.66 us, 6.3 TB/s
 // over the chip.  32 mixed sequences, 138 MB: 83 us without, 77 with the places of the
 // bf16 cache, 63 with those that the times of either kind ask for (chunk_partition.h).
 // The kernel of head_dim 128 keeps 8 registers in scratch for it (36 bytes a lane; two
-// reloads are in the loop over these row tiles' keys); with three steps under way for
-// a wavefront instead of two it would be 20, and 79 us.  A piece starts cold, so
+// reloads are in the loop over these row tiles' keys), and a prompt takes 1 % longer
+// (554 -> 561 on one box); with three steps under way for a wavefront instead of two
+// it would be 20 registers, and 79 us.  A piece starts cold, so
 // contexts of a few tiles gain nothing from their half of the bytes: 160 sequences
 // of one token behind 64 take 32 us (26-27 from the bf16 cache), behind 128 both 35,
 // behind 256 43 against 50, behind 4,096 247 against 406.
